@@ -505,6 +505,105 @@ int alcs_pack_from_csr_device(const int32_t *row_ptr_dev, const int32_t *col_idx
 int alcs_pack_weights_device(const float *W_dev, const uint8_t *mask_dev, int Cout, int Cin, int kernel, int V,
                              const alcs_options *options, void *stream, alcs_packed_t **out);
 
+/*
+ * Feed-forward layers.  Pointwise and fully connected layers beside the sparse ones above: held in four bits
+ * instead of pruned (alcs_mx4_*), and two projections with a gate between them as one layer (alcs_gated_ff),
+ * with its gradients.  Matrices are row-major with one row per image position, token or output channel;
+ * tensors are of one alcs_dtype, 16-bit values are rounded to nearest even, sums are float32 and biases float32.
+ */
+typedef enum alcs_dtype {
+    ALCS_F32 = 0,
+    ALCS_BF16 = 1,
+    ALCS_F16 = 2
+} alcs_dtype;
+
+/*
+ * Microscaled 4-bit storage of a matrix [rows, cols].  A row is cut into blocks of 32 columns, the last of
+ * them padded with zeros, and the number of blocks is padded to a multiple of four with blocks of zeros; with
+ * K = cols rounded up to a multiple of 128:
+ *   scales [rows, K/32]  a byte s per block: its unit is 2^(s - 127).  s = max(floor(log2 max|x|) - 2, -127) + 127,
+ *                        0 for a block of zeros; 255: the block's values are NaN.
+ *   codes  [rows, K/2]   four bits per value, the even column in the low half of a byte: the sign and the
+ *                        position in {0, 0.5, 1, 1.5, 2, 3, 4, 6} of the number nearest to |x| / unit, the even
+ *                        position of two that are equally near, 6 for all beyond.
+ *
+ * alcs_mx4_quantize: X_dev [rows, cols] of `dtype`, rows ldx elements apart (any ldx >= 0), -> codes_dev and
+ *   scales_dev, written completely.  A block that holds an infinity or a NaN gets scale 255 and codes 0.
+ * alcs_mx4_dequantize: the values in `dtype` -> Y_dev [rows, cols]; exact but where the type has no such number.
+ *
+ * Codes are 16-byte, scales 4-byte aligned; cols at most 2^28 (ALCS_E_UNSUPPORTED beyond); rows = 0 is a
+ * no-op.  Asynchronous on `stream`, nothing allocated.
+ */
+int alcs_mx4_quantize(const void *X_dev, long long ldx, long long rows, int cols, int dtype, uint8_t *codes_dev,
+                      uint8_t *scales_dev, void *stream);
+int alcs_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *scales_dev, long long rows, int cols, int dtype,
+                        void *Y_dev, void *stream);
+
+/*
+ * The product of two matrices in that storage, a layer Y = act(X W^T + bias):
+ *   Y[m, n] = act(bias[n] + sum over k of X[m, k] * W[n, k]),  k < K
+ *   X_codes_dev [M, K/2], X_scales_dev [M, K/32]; W_codes_dev [N, K/2], W_scales_dev [N, K/32]; K a multiple
+ *   of 128 (ALCS_E_INVALID_ARG otherwise): stored columns, padding included, which alcs_mx4_quantize fills
+ *   with zeros.  Y_dev [M, N] of `dtype`, fully overwritten; bias_dev [N] float32 or NULL; activation an
+ *   alcs_activation value (NaN gives 0 behind ReLU and ReLU6, as in alcs_sparse_conv_fused).  Products are
+ *   exact, sums float32 (products of blocks whose units multiply to less than 2^-126 may count as zero), Y
+ *   rounded once.  A row of X, or of W, with a NaN block gives a row, or column, of NaN before the activation.
+ *   workspace_dev: NULL, or device memory of at least alcs_mx4_linear_workspace_bytes(M, N, K) bytes, 16-byte
+ *   aligned, the caller's, overwritten: with it, products of few tiles share K out over more workgroups (a
+ *   smaller workspace is not used).  Calls that share one must not overlap.
+ *   M = 0 is a no-op; M, N, K at most 2^28 and 2^31 tiles of 128 x 128 (ALCS_E_UNSUPPORTED beyond).
+ *   Asynchronous on `stream`, nothing allocated; equal calls give equal bits.
+ */
+long long alcs_mx4_linear_workspace_bytes(int M, int N, int K);
+int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scales_dev, const uint8_t *W_codes_dev,
+                    const uint8_t *W_scales_dev, const float *bias_dev, void *Y_dev, int M, int N, int K, int dtype,
+                    int activation, void *workspace_dev, long long workspace_bytes, void *stream);
+
+/* Gates of alcs_gated_ff: the function of the first projection that the second is multiplied with. */
+typedef enum alcs_gate {
+    ALCS_GATE_NONE = 0,      /* g */
+    ALCS_GATE_RELU = 1,      /* max(g, 0), NaN for NaN; derivative 0 at 0 */
+    ALCS_GATE_SILU = 2,      /* g / (1 + exp(-g)) */
+    ALCS_GATE_GELU = 3,      /* g (1 + erf(g / sqrt 2)) / 2 */
+    ALCS_GATE_GELU_TANH = 4, /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
+    ALCS_GATE_SIGMOID = 5    /* 1 / (1 + exp(-g)) */
+} alcs_gate;
+
+/*
+ * The gated feed-forward block in one kernel, like the block of alcs_dw_sparse_conv_fused two layers of which
+ * the intermediates need not be written out:
+ *   G = X Wg^T + bg,  U = X Wu^T + bu,  H = gate(G) * U  (element by element)
+ *   X_dev [T, D], Wg_dev and Wu_dev [F, D] of `dtype`, rows ldx, ldg and ldu elements apart (any pitch >= 0: the
+ *   halves or the alternate rows of one tensor will do); bg_dev, bu_dev [F] float32 or NULL; H_dev [T, F], fully
+ *   overwritten.  G_dev and U_dev [T, F], or both NULL, receive G and U (rounded to `dtype`; H is made from
+ *   the unrounded ones) for the gradients.  gate: an alcs_gate value (ALCS_E_INVALID_ARG otherwise).
+ *   workspace_dev: as for alcs_mx4_linear, alcs_gated_ff_workspace_bytes(T, D, F, dtype) bytes, or NULL.
+ *   T = 0 is a no-op; sizes at most 2^28.  Asynchronous on `stream`, nothing allocated; equal calls give equal
+ *   bits, a row's result may differ in its last bits with the number of rows it is computed with.
+ *
+ * alcs_gated_ff_backward: from dH_dev [T, F], the gradient of a number with respect to H, and the forward's
+ * operands and G, U:
+ *   dU = dH * gate(G),  dG = dH * U * gate'(G)
+ *   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,  dbg, dbu = the sums of dG and dU over the rows
+ *   dX_dev [T, D], dWg_dev and dWu_dev [F, D], dbg_dev and dbu_dev [F], all of `dtype` and fully overwritten; dX,
+ *   the two dW together and the two db together may be NULL.  For 16-bit types dG and dU are rounded to the type
+ *   before the products (the matrix instructions' operands), not for the sums of the biases.
+ *   workspace_dev: device memory of at least alcs_gated_ff_backward_workspace_bytes(T, D, F, dtype) bytes,
+ *   16-byte aligned, the caller's, overwritten (dG and dU live there).  ALCS_E_INVALID_ARG without it.  Calls that
+ *   share one must not overlap.  T = 0 gives gradients of zero.  Everything else as above.
+ *
+ * Outputs must not overlap inputs, the workspace or each other.  The workspace sizes depend on the current device.
+ */
+long long alcs_gated_ff_workspace_bytes(int T, int D, int F, int dtype);
+int alcs_gated_ff(const void *X_dev, long long ldx, const void *Wg_dev, long long ldg, const void *Wu_dev, long long ldu,
+                  const float *bg_dev, const float *bu_dev, void *H_dev, void *G_dev, void *U_dev, int T, int D, int F,
+                  int dtype, int gate, void *workspace_dev, long long workspace_bytes, void *stream);
+long long alcs_gated_ff_backward_workspace_bytes(int T, int D, int F, int dtype);
+int alcs_gated_ff_backward(const void *X_dev, long long ldx, const void *Wg_dev, long long ldg, const void *Wu_dev,
+                           long long ldu, const void *G_dev, const void *U_dev, const void *dH_dev, void *dX_dev,
+                           void *dWg_dev, void *dWu_dev, void *dbg_dev, void *dbu_dev, int T, int D, int F, int dtype,
+                           int gate, void *workspace_dev, long long workspace_bytes, void *stream);
+
 /* What the last alcs_sparse_conv call of this thread launched: fills up to `cap`
  * ints {mode (1 = all input channels resident in LDS, 2 = chunked, 3 = 3x3,
  * 4 = persistent double-buffered with the weights in LDS, 5 = pipelined persistent,

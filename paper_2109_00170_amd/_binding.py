@@ -40,6 +40,8 @@ EXPORTS = [
     "alcs_pack_workspace_bytes", "alcs_pack_network_device", "alcs_packed_add_bf16_weights",
     "alcs_sparse_conv_bf16_mfma",
     "alcs_last_launch", "alcs_latency_estimate", "alcs_network_latency",
+    "alcs_mx4_quantize", "alcs_mx4_dequantize", "alcs_mx4_linear_workspace_bytes", "alcs_mx4_linear",
+    "alcs_gated_ff_workspace_bytes", "alcs_gated_ff", "alcs_gated_ff_backward_workspace_bytes", "alcs_gated_ff_backward",
 ]
 
 
@@ -115,6 +117,9 @@ def load_library():
     lib.alcs_last_launch.argtypes = [cip, ci]
     lib.alcs_select_workspace_bytes.restype = ctypes.c_size_t
     lib.alcs_pack_workspace_bytes.restype = ctypes.c_longlong
+    for f, n in ((lib.alcs_mx4_linear_workspace_bytes, 3), (lib.alcs_gated_ff_workspace_bytes, 4),
+                 (lib.alcs_gated_ff_backward_workspace_bytes, 4)):
+        f.restype, f.argtypes = ctypes.c_longlong, [ci] * n
     spec = importlib.util.spec_from_file_location(__package__ + "._launch", _LAUNCH_PATH)
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
@@ -618,3 +623,85 @@ def alcs_pack_network_device(Ws, masks, Vs, options=None, workspace=None, stream
 def alcs_pack_on_device(W_dev, mask_dev, V: int, options=None) -> Packed:
     """Device weights and flags -> handle without the host seeing weights, flags or layout."""
     return alcs_pack_weights_device(W_dev, mask_dev, V, options=options)
+
+
+# --------------------------------------------------------------------------- feed-forward layers
+
+
+def _workspace_bytes(name, *sizes) -> int:
+    if any(int(s) != s or s > 0x7fffffff for s in sizes):
+        raise ValueError("%s: sizes must be integers of 32 bits, got %r" % (name, sizes))
+    n = int(getattr(load_library(), name)(*(int(s) for s in sizes)))
+    if n < 0:
+        raise AlcsError(n, name)
+    return n
+
+
+def _dtype_code(dtype) -> int:
+    names = ["torch.float32", "torch.bfloat16", "torch.float16"]
+    if str(dtype) not in names:
+        raise ValueError("the type must be one of %s, got %s" % (", ".join(names), dtype))
+    return names.index(str(dtype))
+
+
+def alcs_mx4_quantize(X, codes=None, scales=None, stream=None):
+    """Microscaled 4-bit storage of the matrix X [rows, cols] (float32, bfloat16 or float16, rows any distance
+    apart): returns (codes uint8 [rows, K/2], scales uint8 [rows, K/32]), K = cols rounded up to a multiple of
+    128; allocated here unless given."""
+    if codes is None or scales is None:
+        import torch
+        if X.ndim != 2:
+            raise ValueError("X must be a matrix, got %r" % (tuple(X.shape),))
+        K = (X.shape[1] + 127) // 128 * 128
+        with torch.cuda.stream(_as_stream(stream, X.device)):   # the allocator's stream is the one that writes
+            if codes is None:
+                codes = torch.empty((X.shape[0], K // 2), dtype=torch.uint8, device=X.device)
+            if scales is None:
+                scales = torch.empty((X.shape[0], K // 32), dtype=torch.uint8, device=X.device)
+    _launch.mx4_quantize(X, codes, scales, stream)
+    return codes, scales
+
+
+def _as_stream(stream, device):
+    import torch
+    if stream is None or hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def alcs_mx4_dequantize(codes, scales, Y, stream=None) -> None:
+    """The values that codes and scales stand for, in the type of the contiguous matrix Y [rows, cols]."""
+    return _launch.mx4_dequantize(codes, scales, Y, stream)
+
+
+def alcs_mx4_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    """What alcs_mx4_linear can use on the current GPU for M rows, N columns and K stored columns (twice the
+    width of codes)."""
+    return _workspace_bytes("alcs_mx4_linear_workspace_bytes", M, N, K)
+
+
+def alcs_mx4_linear(X_codes, X_scales, W_codes, W_scales, bias, Y, activation=None, workspace=None, stream=None) -> None:
+    """Y [M, N] = act(X W^T + bias) for X [M, K] and W [N, K] in 4-bit storage; bias float32 or None; activation
+    None, "relu", "relu6" or an alcs_activation integer; workspace a uint8 tensor or None."""
+    return _launch.mx4_linear(X_codes, X_scales, W_codes, W_scales, bias, Y, activation, workspace, stream)
+
+
+def alcs_gated_ff_workspace_bytes(T: int, D: int, F: int, dtype) -> int:
+    return _workspace_bytes("alcs_gated_ff_workspace_bytes", T, D, F, _dtype_code(dtype))
+
+
+def alcs_gated_ff(X, Wg, Wu, bg, bu, H, gate="silu", G=None, U=None, workspace=None, stream=None) -> None:
+    """H [T, F] = gate(G) * U with G = X Wg^T + bg and U = X Wu^T + bu: X [T, D], Wg and Wu [F, D] of one type (rows any
+    distance apart), bg and bu float32 or None; gate "none", "relu", "silu", "gelu", "gelu_tanh", "sigmoid" or an
+    alcs_gate integer.  G and U, where given, are written for alcs_gated_ff_backward."""
+    return _launch.gated_ff(X, Wg, Wu, bg, bu, H, gate, G, U, workspace, stream)
+
+
+def alcs_gated_ff_backward_workspace_bytes(T: int, D: int, F: int, dtype) -> int:
+    return _workspace_bytes("alcs_gated_ff_backward_workspace_bytes", T, D, F, _dtype_code(dtype))
+
+
+def alcs_gated_ff_backward(X, Wg, Wu, G, U, dH, dX, dWg, dWu, dbg, dbu, gate="silu", workspace=None, stream=None) -> None:
+    """The gradients dX [T, D], dWg and dWu [F, D], dbg and dbu [F] (dX, both dW, both db may be None) from dH [T, F] and
+    what alcs_gated_ff was given and wrote; workspace: a uint8 tensor of alcs_gated_ff_backward_workspace_bytes."""
+    return _launch.gated_ff_backward(X, Wg, Wu, G, U, dH, dX, dWg, dWu, dbg, dbu, gate, workspace, stream)

@@ -7,6 +7,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -28,6 +29,11 @@ decltype(&alcs_depthwise_conv) p_depthwise = nullptr;
 decltype(&alcs_dw_sparse_conv_fused) p_dw = nullptr;
 decltype(&alcs_block_scores) p_scores = nullptr;
 decltype(&alcs_pack_network_device) p_pack_network = nullptr;
+decltype(&alcs_mx4_quantize) p_quantize = nullptr;
+decltype(&alcs_mx4_dequantize) p_dequantize = nullptr;
+decltype(&alcs_mx4_linear) p_mx4_linear = nullptr;
+decltype(&alcs_gated_ff) p_gated = nullptr;
+decltype(&alcs_gated_ff_backward) p_gated_backward = nullptr;
 PyObject *g_error = nullptr;  // AlcsError(status, where)
 PyObject *s_ptr = nullptr, *s_cuda_stream = nullptr;
 
@@ -362,6 +368,212 @@ PyObject *pack_network(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return list;
 }
 
+// ---- feed-forward layers: matrices of three types, rows that may lie apart, all on one GPU that need not be
+// the current one
+
+struct Matrices {
+    int device = -1;
+    at::ScalarType type = at::kFloat;
+    bool typed = false;
+
+    // The tensor's place: on the GPU the others are on.
+    bool here(const at::Tensor &t, const char *name) {
+        if (device < 0) device = t.get_device();
+        if (device == t.get_device()) return true;
+        PyErr_Format(PyExc_ValueError, "%s is on another GPU than the tensors before it", name);
+        return false;
+    }
+    // [rows, cols] of the call's type (the first one's: float32, bfloat16 or float16), neighbouring columns next to
+    // each other; rows any distance apart where `strided`, else packed.
+    bool matrix(PyObject *o, const char *name, bool none_ok, bool strided, Arg &a) {
+        if (o == Py_None && none_ok) return true;
+        const bool is = o != Py_None && THPVariable_Check(o);
+        if (is) {
+            const at::Tensor &t = THPVariable_Unpack(o);
+            if (!typed && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf)) {
+                type = t.scalar_type();
+                typed = true;
+            }
+            if (t.is_cuda() && t.layout() == at::kStrided && t.dim() == 2 && typed && t.scalar_type() == type &&
+                (strided ? t.size(1) <= 1 || t.stride(1) == 1 : t.is_contiguous())) {
+                if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) {
+                    PyErr_Format(PyExc_ValueError, "%s: a dimension is more than the library takes", name);
+                    return false;
+                }
+                if (!here(t, name)) return false;
+                a.t = &t;
+                a.p = t.data_ptr();
+                return true;
+            }
+        }
+        PyErr_Format(PyExc_ValueError, "%s must be a matrix on the GPU, %s, of type %s", name,
+                     strided ? "neighbouring columns next to each other" : "contiguous",
+                     typed ? c10::toString(type) : "float32, bfloat16 or float16");
+        return false;
+    }
+    // a contiguous tensor of another type
+    bool other(PyObject *o, const char *name, at::ScalarType want, bool none_ok, Arg &a) {
+        return tensor(o, name, want, none_ok, a) && (!a.t || here(*a.t, name));
+    }
+    // `n` values of the call's type
+    bool vector(PyObject *o, const char *name, int64_t n, Arg &a) {
+        if (!other(o, name, type, true, a)) return false;
+        if (!a.t || a.t->numel() == n) return true;
+        PyErr_Format(PyExc_ValueError, "%s must have %lld entries, got %lld", name, (long long)n, (long long)a.t->numel());
+        return false;
+    }
+    // codes [rows, K/2] and scales [rows, K/32]
+    bool stored(PyObject *co, PyObject *so, const char *codes, const char *scales, Arg &c, Arg &s) {
+        if (!other(co, codes, at::kByte, false, c) || !other(so, scales, at::kByte, false, s)) return false;
+        if (c.t->dim() != 2 || s.t->dim() != 2 || c.dim(1) <= 0 || c.dim(1) % 64 || c.dim(0) != s.dim(0) || s.dim(1) != c.dim(1) / 16) {
+            PyErr_Format(PyExc_ValueError, "%s must be [rows, K/2] with K a multiple of 128, and %s [rows, K/32]", codes, scales);
+            return false;
+        }
+        if (c.dim(1) <= INT32_MAX / 2) return true;
+        PyErr_Format(PyExc_ValueError, "%s: a dimension is more than the library takes", codes);
+        return false;
+    }
+    int dtype() const { return type == at::kFloat ? ALCS_F32 : type == at::kBFloat16 ? ALCS_BF16 : ALCS_F16; }
+    // None: PyTorch's current stream of the tensors' GPU
+    bool stream(PyObject *o, void *&st) const {
+        if (o != Py_None) return stream_of(o, st);
+        st = (void *)c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream();
+        return true;
+    }
+    c10::Device place() const { return c10::Device(c10::DeviceType::CUDA, (c10::DeviceIndex)device); }
+};
+// elements from one row to the next; whatever a tensor of one row says, its only row starts at 0
+long long pitch(const Arg &a) { return a.dim(0) > 1 ? (long long)a.t->stride(0) : (long long)a.dim(1); }
+long long bytes(const Arg &a) { return a.t ? (long long)a.t->numel() : 0; }
+
+// an alcs_gate by its name or number
+bool gate(PyObject *o, int &v) {
+    static const char *const names[] = {"none", "relu", "silu", "gelu", "gelu_tanh", "sigmoid"};
+    if (PyUnicode_Check(o)) {
+        const char *s = PyUnicode_AsUTF8(o);
+        if (!s) return false;
+        for (v = 0; v < 6; ++v)
+            if (!std::strcmp(s, names[v])) return true;
+        PyErr_SetObject(PyExc_KeyError, o);
+        return false;
+    }
+    if (!PyLong_Check(o)) { PyErr_SetObject(PyExc_KeyError, o); return false; }
+    return integer(o, v);
+}
+
+// X, codes, scales, stream
+PyObject *mx4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!count(n, 4)) return nullptr;
+    Matrices m;
+    Arg X, C, S;
+    void *st = nullptr;
+    if (!m.matrix(a[0], "X", false, true, X) || !m.stored(a[1], a[2], "codes", "scales", C, S)) return nullptr;
+    if (C.dim(0) != X.dim(0) || C.dim(1) != (X.dim(1) + 127) / 128 * 64) {
+        PyErr_SetString(PyExc_ValueError, "codes and scales do not have the shapes that X asks for");
+        return nullptr;
+    }
+    if (!m.stream(a[3], st)) return nullptr;
+    const c10::DeviceGuard on(m.place());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_quantize(X.p, pitch(X), X.dim(0), (int)X.dim(1), m.dtype(), (uint8_t *)C.p, (uint8_t *)S.p, st);
+    Py_END_ALLOW_THREADS
+    return done(rc, "alcs_mx4_quantize");
+}
+
+// codes, scales, Y, stream
+PyObject *mx4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!count(n, 4)) return nullptr;
+    Matrices m;
+    Arg C, S, Y;
+    void *st = nullptr;
+    if (!m.stored(a[0], a[1], "codes", "scales", C, S) || !m.matrix(a[2], "Y", false, false, Y)) return nullptr;
+    if (C.dim(0) != Y.dim(0) || C.dim(1) != (Y.dim(1) + 127) / 128 * 64) {
+        PyErr_SetString(PyExc_ValueError, "Y does not have the shape that codes and scales ask for");
+        return nullptr;
+    }
+    if (!m.stream(a[3], st)) return nullptr;
+    const c10::DeviceGuard on(m.place());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_dequantize((const uint8_t *)C.p, (const uint8_t *)S.p, Y.dim(0), (int)Y.dim(1), m.dtype(), Y.p, st);
+    Py_END_ALLOW_THREADS
+    return done(rc, "alcs_mx4_dequantize");
+}
+
+// X codes, X scales, W codes, W scales, bias, Y, activation, workspace, stream
+PyObject *mx4_linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!count(n, 9)) return nullptr;
+    Matrices m;
+    Arg Xc, Xs, Wc, Ws, bias, Y, ws;
+    int act = 0;
+    void *st = nullptr;
+    if (!m.stored(a[0], a[1], "X_codes", "X_scales", Xc, Xs) || !m.stored(a[2], a[3], "W_codes", "W_scales", Wc, Ws) ||
+        !m.other(a[4], "bias", at::kFloat, true, bias) || !m.matrix(a[5], "Y", false, false, Y) || !activation(a[6], act) ||
+        !m.other(a[7], "workspace", at::kByte, true, ws))
+        return nullptr;
+    if (Xc.dim(1) != Wc.dim(1)) { PyErr_SetString(PyExc_ValueError, "X and W do not have the same number of columns"); return nullptr; }
+    if (!shape(Y, "Y", {Xc.dim(0), Wc.dim(0)}) || !per_channel(bias, "bias", Wc.dim(0)) || !m.stream(a[8], st)) return nullptr;
+    const c10::DeviceGuard on(m.place());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_mx4_linear((const uint8_t *)Xc.p, (const uint8_t *)Xs.p, (const uint8_t *)Wc.p, (const uint8_t *)Ws.p, (const float *)bias.p,
+                      Y.p, (int)Xc.dim(0), (int)Wc.dim(0), (int)Xc.dim(1) * 2, m.dtype(), act, ws.p, bytes(ws), st);
+    Py_END_ALLOW_THREADS
+    return done(rc, "alcs_mx4_linear");
+}
+
+// X, Wg, Wu, bg, bu, H, gate, G, U, workspace, stream
+PyObject *gated_ff(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!count(n, 11)) return nullptr;
+    Matrices m;
+    Arg X, Wg, Wu, bg, bu, H, G, U, ws;
+    int kind = 0;
+    void *st = nullptr;
+    if (!m.matrix(a[0], "X", false, true, X) || !m.matrix(a[1], "Wg", false, true, Wg) || !m.matrix(a[2], "Wu", false, true, Wu) ||
+        !m.other(a[3], "bg", at::kFloat, true, bg) || !m.other(a[4], "bu", at::kFloat, true, bu) ||
+        !m.matrix(a[5], "H", false, false, H) || !gate(a[6], kind) || !m.matrix(a[7], "G", true, false, G) ||
+        !m.matrix(a[8], "U", true, false, U) || !m.other(a[9], "workspace", at::kByte, true, ws))
+        return nullptr;
+    const int64_t T = X.dim(0), D = X.dim(1), F = Wg.dim(0);
+    if (!shape(Wg, "Wg", {F, D}) || !shape(Wu, "Wu", {F, D}) || !shape(H, "H", {T, F}) || !shape(G, "G", {T, F}) ||
+        !shape(U, "U", {T, F}) || !per_channel(bg, "bg", F) || !per_channel(bu, "bu", F) || !m.stream(a[10], st))
+        return nullptr;
+    const c10::DeviceGuard on(m.place());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_gated(X.p, pitch(X), Wg.p, pitch(Wg), Wu.p, pitch(Wu), (const float *)bg.p, (const float *)bu.p, H.p, G.p, U.p, (int)T, (int)D,
+                 (int)F, m.dtype(), kind, ws.p, bytes(ws), st);
+    Py_END_ALLOW_THREADS
+    return done(rc, "alcs_gated_ff");
+}
+
+// X, Wg, Wu, G, U, dH, dX, dWg, dWu, dbg, dbu, gate, workspace, stream
+PyObject *gated_ff_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (!count(n, 14)) return nullptr;
+    Matrices m;
+    Arg X, Wg, Wu, G, U, dH, dX, dWg, dWu, dbg, dbu, ws;
+    int kind = 0;
+    void *st = nullptr;
+    if (!m.matrix(a[0], "X", false, true, X) || !m.matrix(a[1], "Wg", false, true, Wg) || !m.matrix(a[2], "Wu", false, true, Wu) ||
+        !m.matrix(a[3], "G", false, false, G) || !m.matrix(a[4], "U", false, false, U) || !m.matrix(a[5], "dH", false, false, dH) ||
+        !m.matrix(a[6], "dX", true, false, dX) || !m.matrix(a[7], "dWg", true, false, dWg) || !m.matrix(a[8], "dWu", true, false, dWu))
+        return nullptr;
+    const int64_t T = X.dim(0), D = X.dim(1), F = Wg.dim(0);
+    if (!shape(Wg, "Wg", {F, D}) || !shape(Wu, "Wu", {F, D}) || !shape(G, "G", {T, F}) || !shape(U, "U", {T, F}) ||
+        !shape(dH, "dH", {T, F}) || !shape(dX, "dX", {T, D}) || !shape(dWg, "dWg", {F, D}) || !shape(dWu, "dWu", {F, D}) ||
+        !m.vector(a[9], "dbg", F, dbg) || !m.vector(a[10], "dbu", F, dbu) || !gate(a[11], kind) ||
+        !m.other(a[12], "workspace", at::kByte, true, ws) || !m.stream(a[13], st))
+        return nullptr;
+    const c10::DeviceGuard on(m.place());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = p_gated_backward(X.p, pitch(X), Wg.p, pitch(Wg), Wu.p, pitch(Wu), G.p, U.p, dH.p, dX.p, dWg.p, dWu.p, dbg.p, dbu.p, (int)T,
+                          (int)D, (int)F, m.dtype(), kind, ws.p, bytes(ws), st);
+    Py_END_ALLOW_THREADS
+    return done(rc, "alcs_gated_ff_backward");
+}
+
 // error class, {name: address}
 PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!count(n, 2)) return nullptr;
@@ -374,7 +586,9 @@ PyObject *connect(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (!get("alcs_sparse_conv", p_sparse) || !get("alcs_sparse_conv_fused", p_fused) || !get("alcs_sparse_conv_bf16", p_bf16) ||
         !get("alcs_sparse_conv_bf16_mfma", p_mfma16) || !get("alcs_dense_conv", p_dense) ||
         !get("alcs_depthwise_conv", p_depthwise) || !get("alcs_dw_sparse_conv_fused", p_dw) || !get("alcs_block_scores", p_scores) ||
-        !get("alcs_pack_network_device", p_pack_network))
+        !get("alcs_pack_network_device", p_pack_network) || !get("alcs_mx4_quantize", p_quantize) ||
+        !get("alcs_mx4_dequantize", p_dequantize) || !get("alcs_mx4_linear", p_mx4_linear) || !get("alcs_gated_ff", p_gated) ||
+        !get("alcs_gated_ff_backward", p_gated_backward))
         return nullptr;
     Py_INCREF(a[0]);
     Py_XDECREF(g_error);
@@ -403,7 +617,9 @@ PyObject *guarded(PyObject *self, PyObject *const *a, Py_ssize_t n) noexcept {
 PyMethodDef methods[] = {ENTRY(connect),        ENTRY(sparse_conv),          ENTRY(sparse_conv_fused),
                          ENTRY(sparse_conv_bf16), ENTRY(sparse_conv_bf16_mfma), ENTRY(dense_conv),
                          ENTRY(depthwise_conv), ENTRY(dw_sparse_conv_fused), ENTRY(block_scores),
-                         ENTRY(packed_info),    ENTRY(pack_network),         {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(packed_info),    ENTRY(pack_network),         ENTRY(mx4_quantize),
+                         ENTRY(mx4_dequantize), ENTRY(mx4_linear),           ENTRY(gated_ff),
+                         ENTRY(gated_ff_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_launch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,194 @@
+"""Microscaled 4-bit storage and the product of two matrices held in it, against float64 from the definition."""
+import math
+
+import pytest
+import torch
+
+import paper_2109_00170_amd as alcs
+from ff_util import check, guarded, linear_ref, padded, quantize_ref, stored64
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def values(rows, cols, seed, dtype=torch.float32, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(rows, cols, generator=g) * std * torch.exp2(torch.randint(-6, 7, (rows, cols), generator=g))).to(dtype)
+
+
+def same_storage(x):
+    c, s = alcs.alcs_mx4_quantize(x)
+    rc, rs = quantize_ref(x.float())
+    assert torch.equal(s.cpu(), rs)
+    assert torch.equal(c.cpu(), rc)
+    return c, s
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 31), (3, 32), (2, 33), (5, 127), (4, 128), (7, 129), (33, 200), (1, 2048), (130, 1111)])
+def test_storage_and_back(rows, cols, dtype):
+    x = values(rows, cols, rows * 1000 + cols, dtype).cuda()
+    c, s = same_storage(x)
+    want = stored64(c, s)[:, :cols]
+    for t in TYPES:
+        y, intact = guarded(rows, cols, dtype=t)
+        alcs.alcs_mx4_dequantize(c, s, y)
+        assert torch.equal(y, want.to(t)) and intact()
+
+
+def test_borders_ties_and_signs():
+    # a block whose unit is 1 and elements on, just below and just above every border, of both signs
+    b = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.9])
+    near = torch.cat([b, torch.nextafter(b, torch.tensor(0.0)), torch.nextafter(b, torch.tensor(9.0))])
+    for unit in (2.0 ** -126, 2.0 ** -120, 2.0 ** -13, 1.0, 2.0 ** 100, 2.0 ** 125):
+        for sign in (1, -1):
+            x = torch.zeros(1, 32)
+            x[0, :27] = near * sign
+            x[0, 27], x[0, 28] = 4.0, -0.0
+            same_storage((x.double() * unit).float().cuda())
+
+
+def test_small_and_extreme_numbers():
+    x = torch.zeros(8, 64)
+    x[0, 0] = 2.0 ** -149                      # the smallest subnormal number
+    x[1, :4] = torch.tensor([2.0 ** -126, 2.0 ** -127, -2.0 ** -128, 3 * 2.0 ** -128])
+    x[2, 0] = 2.0 ** -125
+    x[3, :3] = torch.tensor([3.4e38, -3.4e38, 1e38])
+    x[4, 5] = -0.0
+    x[5, 33] = 1e-30
+    c, s = same_storage(x.cuda())
+    y = torch.empty(8, 64, device="cuda")
+    alcs.alcs_mx4_dequantize(c, s, y)
+    assert torch.equal(y.double(), stored64(c, s)[:, :64])
+    h = torch.zeros(2, 40, dtype=torch.float16)
+    h[0, :3] = torch.tensor([6e-8, -2e-7, 3e-5], dtype=torch.float16)
+    h[1, :2] = torch.tensor([65504.0, -1.0], dtype=torch.float16)
+    same_storage(h.cuda())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_blocks_that_are_not_finite(dtype):
+    x = values(4, 96, 5, dtype)
+    x[0, 3], x[1, 40], x[2, 95] = math.inf, math.nan, -math.inf
+    x = x.cuda()
+    c, s = same_storage(x)
+    y = torch.empty(4, 96, dtype=dtype, device="cuda")
+    alcs.alcs_mx4_dequantize(c, s, y)
+    bad = torch.zeros(4, 96, dtype=torch.bool)
+    bad[0, :32] = bad[1, 32:64] = bad[2, 64:] = True
+    assert torch.equal(torch.isnan(y).cpu(), bad)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_apart_unaligned_and_repeated(dtype):
+    base = values(20, 301, 9, dtype).cuda()
+    for x in (base[:, 1:], base[:, 3:260], base[::2], base[5:6], base[2:3].expand(7, 301), base[:0]):
+        c, s = alcs.alcs_mx4_quantize(x)
+        rc, rs = quantize_ref(x.contiguous())
+        assert torch.equal(c.cpu(), rc) and torch.equal(s.cpu(), rs)
+
+
+def stored(rows, cols, seed):
+    return alcs.alcs_mx4_quantize(values(rows, cols, seed, std=0.2).cuda())
+
+
+def workspace(M, N, K):
+    return torch.empty(alcs.alcs_mx4_linear_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+
+
+# rows: a token, all forms for few rows and their borders, tiles of 128 (with K shared out) and of 256
+SIZES = [(1, 1, 1), (1, 1000, 2048), (2, 17, 129), (16, 64, 512), (17, 33, 600), (33, 15, 128), (64, 130, 1100), (65, 1, 128),
+         (65, 129, 640), (128, 128, 256), (200, 257, 4100), (129, 500, 384), (300, 1000, 1000), (2900, 2901, 390), (2817, 2817, 256)]
+
+
+@pytest.mark.parametrize("i", range(len(SIZES)))
+def test_product(i):
+    M, N, cols = SIZES[i]
+    dtype, act = TYPES[i % 3], ["none", "relu", "relu6"][i // 2 % 3]
+    (xc, xs), (wc, ws) = stored(M, cols, 100 + i), stored(N, cols, 200 + i)
+    bias = None if i % 4 == 1 else torch.randn(N, generator=torch.Generator().manual_seed(i)).cuda()
+    ref, tol = linear_ref(xc, xs, wc, ws, bias, act)
+    for w in (None, workspace(M, N, padded(cols))):
+        y, intact = guarded(M, N, dtype=dtype)
+        alcs.alcs_mx4_linear(xc, xs, wc, ws, bias, y, activation=act, workspace=w)
+        check(y, ref, tol, "product %s" % (SIZES[i],))
+        assert intact()
+
+
+@pytest.mark.parametrize("M", [3, 40, 150])
+def test_product_of_blocks_that_are_not_finite(M):
+    x, w = values(M, 300, 1, std=0.2), values(70, 300, 2, std=0.2)
+    x[M - 1, 290], w[5, 0] = math.nan, math.inf
+    (xc, xs), (wc, ws) = alcs.alcs_mx4_quantize(x.cuda()), alcs.alcs_mx4_quantize(w.cuda())
+    y = torch.zeros(M, 70, device="cuda")
+    alcs.alcs_mx4_linear(xc, xs, wc, ws, None, y)
+    bad = torch.zeros(M, 70, dtype=torch.bool, device="cuda")
+    bad[M - 1], bad[:, 5] = True, True
+    assert torch.equal(torch.isnan(y), bad)
+    ref, tol = linear_ref(xc, xs, wc, ws, None, "none")
+    check(y[~bad], ref[~bad], tol[~bad], "finite part")
+    alcs.alcs_mx4_linear(xc, xs, wc, ws, None, y, activation="relu")   # NaN gives 0
+    assert bool((y[bad] == 0).all())
+
+
+def test_scales_of_any_size():
+    # products of large and small blocks: every scale byte of a result that float32 holds
+    M, N, cols = 20, 24, 256
+    g = torch.Generator().manual_seed(3)
+    (xc, xs), (wc, ws) = stored(M, cols, 1), stored(N, cols, 2)
+    xs = torch.randint(100, 150, xs.shape, generator=g).to(torch.uint8).cuda()
+    ws = torch.randint(100, 150, ws.shape, generator=g).to(torch.uint8).cuda()
+    y = torch.empty(M, N, device="cuda")
+    alcs.alcs_mx4_linear(xc, xs, wc, ws, None, y)
+    check(y, *linear_ref(xc, xs, wc, ws, None, "none"), "scales")
+
+
+def test_no_rows_and_equal_calls():
+    (xc, xs), (wc, ws) = stored(100, 3000, 1), stored(60, 3000, 2)
+    y = torch.full((0, 60), 1.0, device="cuda")
+    alcs.alcs_mx4_linear(xc[:0], xs[:0], wc, ws, None, y)
+    w = workspace(100, 60, padded(3000))
+    a, b = (torch.empty(100, 60, device="cuda") for _ in range(2))
+    alcs.alcs_mx4_linear(xc, xs, wc, ws, None, a, workspace=w)
+    alcs.alcs_mx4_linear(xc, xs, wc, ws, None, b, workspace=w)
+    assert torch.equal(a, b)
+
+
+def test_streams():
+    s = torch.cuda.Stream()
+    x, w = values(50, 500, 1).cuda(), values(60, 500, 2).cuda()
+    torch.cuda.synchronize()
+    for st in (s, s.cuda_stream):
+        y = torch.empty(50, 60, device="cuda")
+        torch.cuda.synchronize()
+        xc, xs = alcs.alcs_mx4_quantize(x, stream=st)
+        wc, ws = alcs.alcs_mx4_quantize(w, stream=st)
+        alcs.alcs_mx4_linear(xc, xs, wc, ws, None, y, stream=st)
+        s.synchronize()
+        check(y, *linear_ref(xc, xs, wc, ws, None, "none"), "another stream")
+
+
+def test_refusals():
+    x = values(8, 130, 1).cuda()
+    c, s = alcs.alcs_mx4_quantize(x)
+    y = torch.empty(8, 8, device="cuda")
+    V = pytest.raises(ValueError)
+    with V: alcs.alcs_mx4_quantize(x.t())                                  # columns apart
+    with V: alcs.alcs_mx4_quantize(x.double())
+    with V: alcs.alcs_mx4_quantize(x.cpu())
+    with V: alcs.alcs_mx4_quantize(x[0])
+    with V: alcs.alcs_mx4_quantize(x, c[:, :64].contiguous(), s)           # another width
+    with V: alcs.alcs_mx4_quantize(x, c, s[:4])
+    with V: alcs.alcs_mx4_dequantize(c, s, torch.empty(8, 300, device="cuda"))
+    with V: alcs.alcs_mx4_dequantize(c, s, torch.empty(130, 8, device="cuda").t())
+    with V: alcs.alcs_mx4_linear(c, s, c, s, None, y[:4])
+    with V: alcs.alcs_mx4_linear(c[:, :64].contiguous(), s[:, :4].contiguous(), c, s, None, y)
+    with V: alcs.alcs_mx4_linear(c, s, c, s, torch.zeros(7, device="cuda"), y)
+    with V: alcs.alcs_mx4_linear(c, s, c, s, torch.zeros(8, device="cuda", dtype=torch.bfloat16), y)
+    with V: alcs.alcs_mx4_linear(c, s, c, s, None, y, workspace=torch.zeros(64, device="cuda"))
+    with pytest.raises(KeyError): alcs.alcs_mx4_linear(c, s, c, s, None, y, activation="silu")
+    with pytest.raises(alcs.AlcsError): alcs.alcs_mx4_linear(c, s, c, s, None, y, activation=3)
+    odd = torch.zeros(c.numel() + 1, dtype=torch.uint8, device="cuda")[1:].view(c.shape)
+    with pytest.raises(alcs.AlcsError): alcs.alcs_mx4_linear(odd, s, c, s, None, y)
+    with pytest.raises(alcs.AlcsError): alcs.alcs_mx4_linear_workspace_bytes(4, 4, 100)
+    with V: alcs.alcs_mx4_linear_workspace_bytes(4, 2 ** 32 + 4, 128)
