@@ -55,8 +55,8 @@ template <class T> __global__ __launch_bounds__(256) void k_gate_grad(const Grad
                 sg[i] += dg[i];
                 su[i] += du[i];
             }
-            store4((T *)a.dG + (long long)r * a.pitch + c, dg, 4, 1);
-            store4((T *)a.dU + (long long)r * a.pitch + c, du, 4, 1);
+            store4((T *)a.dG + (long long)r * a.pitch + c, dg, 4, 4);
+            store4((T *)a.dU + (long long)r * a.pitch + c, du, 4, 4);
         }
     }
     if (!a.sums) return;
@@ -105,7 +105,8 @@ inline bool aligned_rows(const void *p, long long ld, int columns, int E, int ro
 template <int E> int gated_as(Args a, bool aligned, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     typedef typename TypeOf<E>::type T;
     if (a.M <= kFewRows) return launch_few<E, T, true>(a, aligned, stream);
-    Plan p = plan_tiles(E, aligned, true, a.M, a.N, a.KA, 1, 1, cus);
+    const bool near = aligned && near_rows({a.A[0].pitch, a.B[0].pitch, a.B[1].pitch});
+    Plan p = plan_tiles(E, near, true, a.M, a.N, a.KA, 1, 1, cus);
     if (!workspace || workspace_bytes < p.workspace) { p.splits = 1; p.workspace = 0; }
     return launch_tiles<E, T, false, false, true>(a, p, aligned, workspace, cus, xcds, stream);
 }
@@ -172,9 +173,9 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         a.segs = 2; a.results = 1;
         a.out[0] = b.dX;
         a.ldo = b.D;
-        a.vec = b.D % 4 == 0 && (uintptr_t)b.dX % (4 * sz) == 0;
+        a.vec = store_width({b.dX}, b.D, (int)sz);
         const bool al = aligned_rows(b.Wg, b.ldg, b.D, E, b.F) && aligned_rows(b.Wu, b.ldu, b.D, E, b.F);
-        const Plan p = plan_tiles(E, al, false, b.T, b.D, s.pitch, 2, 1, cus);
+        const Plan p = plan_tiles(E, al && near_rows({pitch, b.ldg * sz, b.ldu * sz}), false, b.T, b.D, s.pitch, 2, 1, cus);
         if ((rc = launch_tiles<E, T, false, true, false>(a, p, al, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
     if (b.dWg) {  // dWg = dG^T X and dWu = dU^T X
@@ -186,9 +187,9 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         a.segs = 1; a.results = 2;
         a.out[0] = b.dWg; a.out[1] = b.dWu;
         a.ldo = b.D;
-        a.vec = b.D % 4 == 0 && ((uintptr_t)b.dWg | (uintptr_t)b.dWu) % (4 * sz) == 0;
+        a.vec = store_width({b.dWg, b.dWu}, b.D, (int)sz);
         const bool al = aligned_rows(b.X, b.ldx, b.D, E, b.T);
-        const Plan p = plan_tiles(E, al, false, b.F, b.D, b.T, 1, 2, cus);
+        const Plan p = plan_tiles(E, al && near_rows({pitch, b.ldx * sz}), false, b.F, b.D, b.T, 1, 2, cus);
         if ((rc = launch_tiles<E, T, true, true, false>(a, p, al, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
     return ALCS_OK;
@@ -242,7 +243,7 @@ extern "C" int alcs_gated_ff(const void *X_dev, long long ldx, const void *Wg_de
     a.out[0] = H_dev; a.pre[0] = G_dev; a.pre[1] = U_dev;
     a.ldo = F;
     a.act = gate;
-    a.vec = F % 4 == 0 && ((uintptr_t)H_dev | (uintptr_t)G_dev | (uintptr_t)U_dev) % (4 * sz) == 0;
+    a.vec = store_width({H_dev, G_dev, U_dev}, F, (int)sz);
     const bool al = aligned_rows(X_dev, ldx, D, dtype, T) && aligned_rows(Wg_dev, ldg, D, dtype, F) &&
                     aligned_rows(Wu_dev, ldu, D, dtype, F);
     const hipStream_t st = (hipStream_t)stream;

@@ -88,7 +88,7 @@ constexpr int kMaxSize = 1 << 28;
 
 template <class T> int linear_as(const Args &a, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     if (a.M <= kFewRows) return launch_few<kMX4, T, false>(a, true, stream);
-    Plan p = plan_tiles(kMX4, true, false, a.M, a.N, a.KA, 1, 1, cus);
+    Plan p = plan_tiles(kMX4, near_rows({a.A[0].pitch}), false, a.M, a.N, a.KA, 1, 1, cus);
     if (!workspace || workspace_bytes < p.workspace) { p.splits = 1; p.workspace = 0; }
     return launch_tiles<kMX4, T, false, false, false>(a, p, true, workspace, cus, xcds, stream);
 }
@@ -173,7 +173,7 @@ extern "C" int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scal
     a.out[0] = Y_dev;
     a.ldo = N;
     a.act = activation;
-    a.vec = N % 4 == 0 && (uintptr_t)Y_dev % (dtype == ALCS_F32 ? 16 : 8) == 0;
+    a.vec = store_width({Y_dev}, N, dtype == ALCS_F32 ? 4 : 2);
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == ALCS_F32) return linear_as<float>(a, workspace_dev, workspace_bytes, cus, xcds, st);
     if (dtype == ALCS_BF16) return linear_as<__bf16>(a, workspace_dev, workspace_bytes, cus, xcds, st);

@@ -21,6 +21,8 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
+#include <type_traits>
 
 #include "alcs_internal.h"
 
@@ -66,6 +68,22 @@ template <bool EXACT> __device__ inline float gate_value(int gate, float g) {
         case ALCS_GATE_SIGMOID: return sigmoid<EXACT>(g);
         default: return g;
     }
+}
+// eight of them: one look at which gate it is
+template <bool EXACT> __device__ inline void gate_values(int gate, const float (&g)[8], float (&v)[8]) {
+#define ALCS_EACH(kind)                                                        \
+    case kind:                                                                 \
+        _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] = gate_value<EXACT>(kind, g[e]); \
+        break;
+    switch (gate) {
+        ALCS_EACH(ALCS_GATE_NONE)
+        ALCS_EACH(ALCS_GATE_RELU)
+        ALCS_EACH(ALCS_GATE_SILU)
+        ALCS_EACH(ALCS_GATE_GELU)
+        ALCS_EACH(ALCS_GATE_GELU_TANH)
+        ALCS_EACH(ALCS_GATE_SIGMOID)
+    }
+#undef ALCS_EACH
 }
 // value and derivative
 template <bool EXACT> __device__ inline void gate_both(int gate, float g, float &v, float &d) {
@@ -115,7 +133,7 @@ struct Args {
     void *pre[2];        // gated: G and U where the caller keeps them, or null
     long long ldo;       // elements from one row of out (and pre) to the next
     int act;             // alcs_activation, or alcs_gate for a gated product
-    int vec;             // rows of out and pre may be written four elements at a time
+    int vec;             // elements that out and pre may be written at a time: 8, 4 or 1
 };
 
 __device__ const v4i g_zeros[4] = {};  // what pieces beyond K read
@@ -292,10 +310,31 @@ template <int E> __device__ inline v4f multiply(v4i b, v4i a, v4f c, int s, int 
     }
 }
 
+// The same on accumulators that stay where they are (in accumulation registers): left to itself the compiler
+// moves 256 of them about in the loop of k_big.  Whoever reads a result first passes matrix_done().
+template <int E, int S> __device__ inline void multiply_in_place(v4f &c, v4i b, v4i a, int sb, int sa) {
+    if (E == kBF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
+    else if (E == kF16) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
+    else if (S == 0)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+    else
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+}
+// A register that a vector instruction wrote may be a matrix instruction's operand two states later.
+__device__ inline void operands_ready() { asm volatile("s_nop 1"); }
+// The last matrix instruction writes its result within 16 passes of four cycles.
+template <int FM, int FN> __device__ inline void matrix_done(v4f (&acc)[FM][FN]) {
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
+}
+
 // ------------------------------------------------------------------------------ what follows the sum
 
 template <class T> __device__ inline void store4(T *p, const float v[4], int n, int vec) {
-    if (vec && n >= 4) {
+    if (vec >= 4 && n >= 4) {
         struct alignas(sizeof(T) * 4) Four { T e[4]; } f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f.e[i] = (T)v[i];
@@ -303,6 +342,18 @@ template <class T> __device__ inline void store4(T *p, const float v[4], int n, 
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = (T)v[i];
+    }
+}
+template <class T> __device__ inline void store8(T *p, const float v[8], int n, int vec) {
+    if (vec == 8 && n >= 8) {
+        struct alignas(16) Eight { T e[8]; } f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.e[i] = (T)v[i];
+        *(Eight *)p = f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
             if (i < n) p[i] = (T)v[i];
     }
 }
@@ -330,6 +381,102 @@ template <class T> __device__ inline void finish_gated(const Args &a, long long 
     if (a.pre[0]) {
         store4((T *)a.pre[0] + at, gg, left, a.vec);
         store4((T *)a.pre[1] + at, uu, left, a.vec);
+    }
+}
+
+// a wavefront's accumulators, rows from m0 and columns (of both projections where GATED) from n0 on
+template <class T, int FM, int FN, bool GATED>
+__device__ inline void finish_tile(const Args &a, const v4f (&acc)[FM][FN], int m0, int n0, int result, int split, int lane) {
+    const int r = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int m = m0 + i * 16 + r;
+        if (m >= a.M) continue;
+        if (GATED) {
+#pragma unroll
+            for (int j = 0; j < FN / 2; ++j) {
+                const int n = n0 + j * 16 + q * 4;
+                const v4f gv = acc[i][j], uv = acc[i][j + FN / 2];
+                if (a.partial) {
+                    float *p = a.partial + ((long long)split * 2 * a.M + m) * a.N + n;
+                    const float g[4] = {gv[0], gv[1], gv[2], gv[3]}, u[4] = {uv[0], uv[1], uv[2], uv[3]};
+                    if (a.N > n) {
+                        store4(p, g, a.N - n, a.N % 4 == 0 ? 4 : 1);
+                        store4(p + (long long)a.M * a.N, u, a.N - n, a.N % 4 == 0 ? 4 : 1);
+                    }
+                } else {
+                    finish_gated<T>(a, m, n, gv, uv);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int n = n0 + j * 16 + q * 4;
+                const v4f c = acc[i][j];
+                if (a.partial) {
+                    const float v[4] = {c[0], c[1], c[2], c[3]};
+                    if (a.N > n)
+                        store4(a.partial + (((long long)split * a.results + result) * a.M + m) * a.N + n, v, a.N - n, a.N % 4 == 0 ? 4 : 1);
+                } else {
+                    finish_plain<T>(a, result, m, n, c);
+                }
+            }
+        }
+    }
+}
+
+// The same for 128 x 128 accumulators, through the wavefront's 32 KB of LDS, 64 rows at a time, so that the gate
+// is a short loop and a row leaves in 16-byte stores: [row][16-byte piece ^ (row & 7)].
+template <class T, bool GATED>
+__device__ inline void finish_big(const Args &a, const v4f (&acc)[8][8], char *mine, int m0, int n0, int result, int lane) {
+    constexpr bool kExact = sizeof(T) == 4;
+    constexpr int kLanes = GATED ? 8 : 16;  // of a row: eight columns (of both projections) a lane
+    const int r = lane & 15, q = lane >> 4;
+    const int n = n0 + lane % kLanes * 8, left = a.N - n;
+    float b0[8], b1[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        b0[e] = a.bias[0] && e < left ? a.bias[0][n + e] : 0.0f;
+        b1[e] = GATED && a.bias[1] && e < left ? a.bias[1][n + e] : 0.0f;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                *(v4f *)(mine + (i * 16 + r) * 512 + (((j * 4 + q) ^ (r & 7)) << 4)) = acc[half * 4 + i][j];
+#pragma clang loop unroll_count(2)
+        for (int it = 0; it < kLanes; ++it) {
+            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + half * 64 + row;
+            float c[8], u[8], h[8];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int piece = lane % kLanes * 2 + k;
+                const v4f v = *(const v4f *)(mine + row * 512 + ((piece ^ (row & 7)) << 4));
+                const v4f w = GATED ? *(const v4f *)(mine + row * 512 + (((piece + 16) ^ (row & 7)) << 4)) : v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    c[4 * k + e] = v[e] + b0[4 * k + e];
+                    u[4 * k + e] = w[e] + b1[4 * k + e];
+                }
+            }
+            const long long at = m * a.ldo + n;
+            if (GATED) {
+                gate_values<kExact>(a.act, c, h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[e] *= u[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[e] = activate(a.act, c[e]);
+            }
+            if (m >= a.M || left <= 0) continue;
+            store8((T *)a.out[GATED ? 0 : result] + at, h, left, a.vec);
+            if (GATED && a.pre[0]) {
+                store8((T *)a.pre[0] + at, c, left, a.vec);
+                store8((T *)a.pre[1] + at, u, left, a.vec);
+            }
+        }
     }
 }
 
@@ -450,42 +597,225 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(const Args a) {
         }
     }
 
-    const int r = lane & 15, q = lane >> 4;
+    finish_tile<T, FM, FN, GATED>(a, acc, m0 + wm * FM * 16, n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
+}
+
+// ------------------------------------------------------------------------------ large tiles
+
+// 256 x 256, four wavefronts with 128 x 128 each, one per SIMD: what LDS has to deliver falls with the
+// wavefront's tile (at 128 x 64 its reads and the arriving tiles take as many cycles as the matrix instructions).
+// With one wavefront a SIMD nothing else fills its waits, so the loop is laid out by hand: a K tile is two
+// steps of 64 matrix instructions, and during each the fragments of the next step are read.  One barrier a
+// tile, in front of its second step: by then every wavefront has read this tile to its end and the next one has
+// arrived, so the one after that can be sent for into this tile's buffer, a whole tile ahead.
+constexpr int kBigSide = 256;
+constexpr long long kBigPitch = 1 << 22;  // rows so far apart at most that a tile's offsets fit 32 bits
+
+// As Stage, with 32-bit offsets from a base that is the same for all lanes.
+template <int E, bool KSTRIDED> struct BigStage {
+    static constexpr int R = kBigSide, W = 4, kElems = per16(E), kK = 8 * kElems, kLoads = R * kTileBytes / 1024 / W;
+    typedef Stage<E, R, W, KSTRIDED, true> Places;
+    unsigned off[kLoads];
+    const char *base;
+    const char *sbase;
+    unsigned soff[2];
+    template <class F> __device__ void start_rows(int wave, int lane, F row_of, long long pitch) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int m = m0 + (wm * FM + i) * 16 + r;
-        if (m >= a.M) continue;
-        if (GATED) {
-#pragma unroll
-            for (int j = 0; j < FN / 2; ++j) {
-                const int n = n0 + (wn * FN / 2 + j) * 16 + q * 4;
-                if (a.partial) {
-                    float *p = a.partial + ((long long)split * 2 * a.M + m) * a.N + n;
-                    const float g[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                    const v4f uv = acc[i][j + FN / 2];
-                    const float u[4] = {uv[0], uv[1], uv[2], uv[3]};
-                    if (a.N > n) {
-                        store4(p, g, a.N - n, a.N % 4 == 0);
-                        store4(p + (long long)a.M * a.N, u, a.N - n, a.N % 4 == 0);
-                    }
-                } else {
-                    finish_gated<T>(a, m, n, acc[i][j], acc[i][j + FN / 2]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int n = n0 + (wn * FN + j) * 16 + q * 4;
-                if (a.partial) {
-                    const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                    if (a.N > n)
-                        store4(a.partial + (((long long)split * a.results + result) * a.M + m) * a.N + n, v, a.N - n, a.N % 4 == 0);
-                } else {
-                    finish_plain<T>(a, result, m, n, acc[i][j]);
-                }
-            }
+        for (int i = 0; i < kLoads; ++i) {
+            int row, k;
+            Places::place(i, wave, lane, row, k);
+            off[i] = (unsigned)row_of(row) * (unsigned)pitch + k / kElems * 16;
         }
     }
+    __device__ void start_columns(int wave, int lane, unsigned pitch, int left) {  // left: columns from the tile's first on
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int row, k;
+            Places::place(i, wave, lane, row, k);
+            off[i] = k * pitch + (unsigned)min(row, left - kElems) * bytes_of(E);
+        }
+    }
+    template <class F> __device__ void start_scales(int wave, int lane, F row_of, long long pitch) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int d = (wave * 2 + i) * 64 + lane;
+            soff[i] = (unsigned)row_of(((d >> 7) * 4 + (d & 3)) * 16 + ((d >> 3) & 15)) * (unsigned)(pitch / 16) + ((d >> 2) & 1) * 4;
+        }
+    }
+    // load i of the K tile; WHOLE: all of it inside K, else `left` elements are
+    template <bool WHOLE> __device__ void issue(int i, int left, unsigned lds, int wave, int lane) const {
+        const unsigned at = lds + (wave * kLoads + i) * 1024;
+        if (WHOLE) {
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]), "s"(base), "s"(at) : "memory");
+        } else {
+            int row, k, l = lane;
+            asm volatile("" : "+v"(l));  // the last tile's business: nothing of it is kept in registers by the loop
+            Places::place(i, wave, l, row, k);
+            lds_load16(k < left ? base + off[i] : (const char *)g_zeros, at);
+        }
+    }
+    template <bool WHOLE> __device__ void issue_scales(int left, unsigned slds, int wave, int lane) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned at = slds + (wave * 2 + i) * 256;
+            if (WHOLE) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(soff[i]), "s"(sbase), "s"(at) : "memory");
+            else lds_load4(((lane >> 2) & 1) * 128 < left ? sbase + soff[i] : (const char *)g_zeros, at);
+        }
+    }
+};
+
+template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 1) void k_big(const Args a) {
+    constexpr int kA = kBigSide * kTileBytes, kS = E == kMX4 ? kBigSide * 8 : 0, kBuf = 2 * kA + 2 * kS, kK = 8 * per16(E);
+    extern __shared__ __align__(16) char lds[];
+    int tm, tn, z;
+    if (!tile_of(a, tm, tn, z)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int m0 = tm * kBigSide, n0 = tn * (GATED ? kBigSide / 2 : kBigSide);
+    const int result = a.results == 2 ? z : 0;
+    const int all = a.ktiles * a.segs;
+
+    v4f acc[8][8] = {};
+    BigStage<E, AK> sa;
+    BigStage<E, BK> sb;
+    long long stepA = 0, stepB = 0;
+    int next = 0, in_seg = 0;  // the next tile to send for, and its number in its segment
+    unsigned to = lds_offset(lds);
+    auto segment = [&](bool second) {
+        const bool sA = second || result == 1;
+        const long long pitchA = sA ? a.A[1].pitch : a.A[0].pitch;
+        // a gated product's second operand: a wavefront loads rows of one projection
+        const bool sB = GATED ? wave & 1 : second;
+        const long long pitchB = sB ? a.B[1].pitch : a.B[0].pitch;
+        const char *pa = sA ? a.A[1].p : a.A[0].p, *pb = sB ? a.B[1].p : a.B[0].p;
+        if (AK) {
+            sa.base = pa + (long long)m0 * bytes_of(E);
+            stepA = pitchA * kK;
+            sa.start_columns(wave, lane, (unsigned)pitchA, a.A[0].rows - m0);
+        } else {
+            sa.base = pa + m0 * pitchA;
+            stepA = kTileBytes;
+            sa.start_rows(wave, lane, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
+        }
+        if (BK) {
+            sb.base = pb + (long long)n0 * bytes_of(E);
+            stepB = pitchB * kK;
+            sb.start_columns(wave, lane, (unsigned)pitchB, a.B[0].rows - n0);
+        } else {
+            sb.base = pb + n0 * pitchB;
+            stepB = kTileBytes;
+            sb.start_rows(wave, lane, [&](int row) { return min(GATED ? (row >> 7) * 64 + (row & 63) : row, a.N - 1 - n0); }, pitchB);
+        }
+        if (E == kMX4) {
+            sa.sbase = (const char *)a.A[0].scales + m0 * (pitchA / 16);
+            sa.start_scales(wave, lane, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
+            sb.sbase = (const char *)a.B[0].scales + n0 * (pitchB / 16);
+            sb.start_scales(wave, lane, [&](int row) { return min(row, a.N - 1 - n0); }, pitchB);
+        }
+    };
+    // one sixteenth of the loads of tile `next`
+    auto issue = [&](auto whole, int part) {
+        constexpr bool kWhole = decltype(whole)::value;
+        const int leftA = a.KA - in_seg * kK, leftB = a.KB - in_seg * kK;
+        if (part < 8) sa.template issue<kWhole>(part, leftA, to, wave, lane);
+        else sb.template issue<kWhole>(part - 8, leftB, to + kA, wave, lane);
+        if (E == kMX4 && part == 7) sa.template issue_scales<kWhole>(leftA, to + 2 * kA, wave, lane);
+        if (E == kMX4 && part == 15) sb.template issue_scales<kWhole>(leftB, to + 2 * kA + kS, wave, lane);
+    };
+    auto issued = [&] {
+        sa.base += stepA;
+        sb.base += stepB;
+        if (E == kMX4) { sa.sbase += 8; sb.sbase += 8; }
+        ++next;
+        if (++in_seg == a.ktiles && next < all) {
+            in_seg = 0;
+            segment(true);
+        }
+    };
+    const Reader<E, kBigSide, AK> ra(wm * 128, lane);
+    const Reader<E, kBigSide, BK> rb(wn * 128, lane);
+    const unsigned lds0 = to;
+
+    segment(false);
+#pragma unroll
+    for (int part = 0; part < 16; ++part) issue(std::false_type{}, part);
+    issued();
+    wait_loads();
+    __syncthreads();
+    if (next < all) {
+        to = lds0 + kBuf;
+#pragma unroll
+        for (int part = 0; part < 16; ++part) issue(std::false_type{}, part);
+        issued();
+    }
+    v4i pa[8], pb[8], qa[8], qb[8];  // fragments of a first and of a second step
+    int ca[8] = {}, cb[8] = {};      // a tile's scales: step s takes byte s
+    auto scales = [&](const char *here) {
+        if (E != kMX4) return;
+        const int at = ((lane & 15) * 2 + (lane >> 5)) * 16, shift = (lane & 16);
+#pragma unroll
+        for (int f = 0; f < 8; f += 4) {
+            const v4i va = *(const v4i *)(here + 2 * kA + (wm * 8 + f) * 128 + at);
+            const v4i vb = *(const v4i *)(here + 2 * kA + kS + (wn * 8 + f) * 128 + at);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                ca[f + j] = (unsigned)va[j] >> shift;
+                cb[f + j] = (unsigned)vb[j] >> shift;
+            }
+        }
+    };
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+        pa[f] = ra.get(lds, f, 0);
+        pb[f] = rb.get(lds + kA, f, 0);
+    }
+    scales(lds);
+    // A wavefront issues in order, and a matrix instruction keeps its unit busy for four issues: one other
+    // instruction fits behind each without a gap, several in a row do not.
+    for (int t = 0; t < all; ++t) {
+        char *here = lds + (t & 1) * kBuf, *there = lds + (~t & 1) * kBuf;
+        operands_ready();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = i * 8 + j;
+                multiply_in_place<E, 0>(acc[i][j], pb[j], pa[i], cb[j], ca[i]);
+                if (at < 32 && at % 4 == 0) qb[at / 4] = rb.get(here + kA, at / 4, 1);
+                if (at < 32 && at % 4 == 2) qa[at / 4] = ra.get(here, at / 4, 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        int da[8], db[8];
+#pragma unroll
+        for (int f = 0; f < 8; ++f) { da[f] = ca[f]; db[f] = cb[f]; }
+        wait_loads();
+        __syncthreads();
+        const bool more = next < all, whole = more && (in_seg + 1) * kK <= min(a.KA, a.KB);
+        to = lds0 + (t & 1) * kBuf;
+        if (more && !whole) {
+#pragma unroll
+            for (int part = 0; part < 16; ++part) issue(std::false_type{}, part);
+        }
+        operands_ready();
+        // (behind the last tile the fragments are those of an old one, and nobody multiplies them)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = i * 8 + j;
+                multiply_in_place<E, 1>(acc[i][j], qb[j], qa[i], db[j], da[i]);
+                if (at < 32 && at % 4 == 0) pb[at / 4] = rb.get(there + kA, at / 4, 0);
+                if (at < 32 && at % 4 == 2) pa[at / 4] = ra.get(there, at / 4, 0);
+                if (at % 4 == 3 && whole) issue(std::true_type{}, at / 4);
+                if (at == 40) scales(there);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (more) issued();
+    }
+    matrix_done(acc);
+    __syncthreads();
+    finish_big<T, GATED>(a, acc, lds + wave * 32768, m0 + wm * 128, n0 + wn * (GATED ? 64 : 128), result, lane);
 }
 
 // The sums of a split K, added in the order of the splits; a thread has four neighbours of a row.
@@ -611,17 +941,24 @@ __global__ __launch_bounds__(512, 2) void k_few(const Args a) {
 
 // ------------------------------------------------------------------------------ launches
 
+// elements that rows of `columns` packed ones may be written at a time, 0 pointers aside
+inline int store_width(std::initializer_list<const void *> outs, int columns, int size) {
+    uintptr_t all = 0;
+    for (const void *p : outs) all |= (uintptr_t)p;
+    return columns % 8 == 0 && all % 16 == 0 ? 8 : columns % 4 == 0 && all % (4 * size) == 0 ? 4 : 1;
+}
 struct Plan {
     bool big;    // 256 x 256 tiles, eight wavefronts; else 128 x 128, four
     int tiles_m, tiles_n, ktiles, splits;
     long long workspace;  // bytes of sums that a split needs
 };
 // M rows and N columns (of each projection where gated), `results` of them, K elements in each of `segs` segments.
-inline Plan plan_tiles(int E, bool aligned, bool gated, long long M, long long N, long long K, int segs, int results, int cus) {
+// near: the operands are aligned and their rows at most kBigPitch apart.
+inline Plan plan_tiles(int E, bool near, bool gated, long long M, long long N, long long K, int segs, int results, int cus) {
     auto up = [](long long a, long long b) { return (a + b - 1) / b; };
     Plan p{};
     p.ktiles = (int)up(K, 8 * per16(E));
-    p.big = aligned && E != kF32 && up(M, 256) * up(N, gated ? 128 : 256) * results >= cus / 2;
+    p.big = near && E != kF32 && up(M, 256) * up(N, gated ? 128 : 256) * results >= cus / 2;
     const int side = p.big ? 256 : 128;
     p.tiles_m = (int)up(M, side);
     p.tiles_n = (int)up(N, gated ? side / 2 : side);
@@ -633,9 +970,10 @@ inline Plan plan_tiles(int E, bool aligned, bool gated, long long M, long long N
     return p;
 }
 inline long long workspace_of(int E, bool gated, long long M, long long N, long long K, int segs, int results, int cus) {
-    const long long a = plan_tiles(E, true, gated, M, N, K, segs, results, cus).workspace;
-    return E == kMX4 ? a : std::max(a, plan_tiles(E, false, gated, M, N, K, segs, results, cus).workspace);
+    return std::max(plan_tiles(E, true, gated, M, N, K, segs, results, cus).workspace,
+                    plan_tiles(E, false, gated, M, N, K, segs, results, cus).workspace);
 }
+inline bool near_rows(std::initializer_list<long long> pitches) { return std::max(pitches) <= kBigPitch; }
 inline int launched() {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return ALCS_OK;
@@ -652,6 +990,14 @@ int launch_one(Args &a, hipStream_t stream) {
     hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(WM * WN * 64), lds, stream, a);
     return launched();
 }
+template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, hipStream_t stream) {
+    constexpr int lds = 4 * (kBigSide * kTileBytes + (E == kMX4 ? kBigSide * 8 : 0));
+    auto kern = k_big<E, T, AK, BK, GATED>;
+    const int rc = allow_lds((const void *)kern, lds);
+    if (rc != ALCS_OK) return rc;
+    hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(256), lds, stream, a);
+    return launched();
+}
 // The product that `a` describes (operands, sizes, outputs and segs / results set), tiles by `plan`.
 template <int E, class T, bool AK, bool BK, bool GATED>
 int launch_tiles(Args a, const Plan &plan, bool aligned, void *workspace, int cus, int xcds, hipStream_t stream) {
@@ -664,14 +1010,14 @@ int launch_tiles(Args a, const Plan &plan, bool aligned, void *workspace, int cu
     a.per_xcd = (unsigned)((total + xcds - 1) / xcds);
     int rc;
     if constexpr (E == kMX4) {
-        rc = plan.big ? launch_one<E, T, 256, 256, 2, 4, AK, BK, GATED, true>(a, stream)
+        rc = plan.big ? launch_big<E, T, AK, BK, GATED>(a, stream)
                       : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream);
     } else if constexpr (E == kF32) {
         rc = aligned ? launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream)
                      : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, false>(a, stream);
     } else {
         rc = !aligned ? launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, false>(a, stream)
-             : plan.big ? launch_one<E, T, 256, 256, 2, 4, AK, BK, GATED, true>(a, stream)
+             : plan.big ? launch_big<E, T, AK, BK, GATED>(a, stream)
                         : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream);
     }
     if (rc != ALCS_OK || a.splits == 1) return rc;
