@@ -23,6 +23,7 @@
 #include <cstdint>
 #include <initializer_list>
 #include <type_traits>
+#include <utility>
 
 #include "alcs_internal.h"
 
@@ -167,12 +168,15 @@ template <int E, int R, int W, bool KSTRIDED, bool ALIGNED> struct Stage {
     int left[kLoads];   // K strided: elements of the piece inside the operand
     v4i held[ALIGNED ? 1 : kLoads];
 
+    // K contiguous: the 16 bytes of K that piece c of a row holds.  4-bit: a lane reads pieces c and c + 4, and should
+    // find their scales next to each other.
+    static __device__ int block_at(int c) { return E == kMX4 ? (c & 3) * 2 + (c >> 2) : c; }
     // where lane `lane`'s piece of load i lies: row of the tile (K contiguous) or k and first row (K strided)
     static __device__ void place(int i, int wave, int lane, int &row, int &k) {
         const int o = (wave * kLoads + i) * 1024 + lane * 16;
         if (!KSTRIDED) {
             row = o / kTileBytes;
-            k = (((o / 16) & 7) ^ (row & 7)) * kElems;
+            k = block_at(((o / 16) & 7) ^ (row & 7)) * kElems;
         } else {
             constexpr int RB = R * (E == kF32 ? 4 : 2);
             k = o / RB;
@@ -267,8 +271,7 @@ template <int E, int R, bool KSTRIDED> struct Reader {
     __device__ v4i get(const char *lds, int f, int s) const {
         const int r = lane & 15, q = lane >> 4;
         if (!KSTRIDED) {
-            const int piece = E == kMX4 ? 2 * q + s : 4 * s + q;
-            return *(const v4i *)(lds + (first + f * 16 + r) * kTileBytes + ((piece ^ (r & 7)) << 4));
+            return *(const v4i *)(lds + (first + f * 16 + r) * kTileBytes + (((4 * s + q) ^ (r & 7)) << 4));
         }
         constexpr int RB = R * (E == kF32 ? 4 : 2);
         const int u = first / 16 + f;
@@ -310,26 +313,46 @@ template <int E> __device__ inline v4f multiply(v4i b, v4i a, v4f c, int s, int 
     }
 }
 
-// The same on accumulators that stay where they are (in accumulation registers): left to itself the compiler
-// moves 256 of them about in the loop of k_big.  Whoever reads a result first passes matrix_done().
-template <int E, int S> __device__ inline void multiply_in_place(v4f &c, v4i b, v4i a, int sb, int sa) {
-    if (E == kBF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
-    else if (E == kF16) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
-    else if (S == 0)
-        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+// k_big's accumulators: fragment (i, j)'s four values are accumulation registers 4 (8 i + j) and on, by number.  Left
+// to itself the compiler moves 256 of them about inside the loop.  Nothing else in that kernel uses accumulation
+// registers (tests/test_host_matrix_hazards.py reads that, and the distances below, off the built kernels).
+template <int E, int S, int I> __device__ inline void multiply_at(v4i b, v4i a, int sb, int sa) {
+    if constexpr (E == kBF16)
+        asm volatile("v_mfma_f32_16x16x32_bf16 a[%2:%3], %0, %1, a[%2:%3]" ::"v"(b), "v"(a), "i"(4 * I), "i"(4 * I + 3));
+    else if constexpr (E == kF16)
+        asm volatile("v_mfma_f32_16x16x32_f16 a[%2:%3], %0, %1, a[%2:%3]" ::"v"(b), "v"(a), "i"(4 * I), "i"(4 * I + 3));
+    else if constexpr (S == 0)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 a[%4:%5], %0, %1, a[%4:%5], %2, %3 op_sel_hi:[0,0,0] cbsz:4 blgp:4" ::"v"(b), "v"(a), "v"(sb), "v"(sa), "i"(4 * I), "i"(4 * I + 3));
     else
-        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 a[%4:%5], %0, %1, a[%4:%5], %2, %3 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4" ::"v"(b), "v"(a), "v"(sb), "v"(sa), "i"(4 * I), "i"(4 * I + 3));
 }
-// A register that a vector instruction wrote may be a matrix instruction's operand two states later.
+template <int I> __device__ inline void clear_at() {
+    asm volatile("v_accvgpr_write_b32 a[%0], 0\n\tv_accvgpr_write_b32 a[%1], 0\n\tv_accvgpr_write_b32 a[%2], 0\n\tv_accvgpr_write_b32 a[%3], 0"
+                 ::"i"(4 * I), "i"(4 * I + 1), "i"(4 * I + 2), "i"(4 * I + 3));
+}
+template <int I> __device__ inline v4f read_at() {
+    float x, y, z, w;
+    asm volatile("v_accvgpr_read_b32 %0, a[%4]\n\tv_accvgpr_read_b32 %1, a[%5]\n\tv_accvgpr_read_b32 %2, a[%6]\n\tv_accvgpr_read_b32 %3, a[%7]"
+                 : "=v"(x), "=v"(y), "=v"(z), "=v"(w) : "i"(4 * I), "i"(4 * I + 1), "i"(4 * I + 2), "i"(4 * I + 3));
+    return v4f{x, y, z, w};
+}
+// The kernel has all 256: the registers that are named to the compiler.
+#define ALCS_TEN(n) "a" #n "0", "a" #n "1", "a" #n "2", "a" #n "3", "a" #n "4", "a" #n "5", "a" #n "6", "a" #n "7", "a" #n "8", "a" #n "9"
+__device__ inline void claim_accumulators() {
+    asm volatile("" ::: "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", ALCS_TEN(1), ALCS_TEN(2), ALCS_TEN(3), ALCS_TEN(4),
+                 ALCS_TEN(5), ALCS_TEN(6), ALCS_TEN(7), ALCS_TEN(8), ALCS_TEN(9), ALCS_TEN(10), ALCS_TEN(11), ALCS_TEN(12), ALCS_TEN(13),
+                 ALCS_TEN(14), ALCS_TEN(15), ALCS_TEN(16), ALCS_TEN(17), ALCS_TEN(18), ALCS_TEN(19), ALCS_TEN(20), ALCS_TEN(21),
+                 ALCS_TEN(22), ALCS_TEN(23), ALCS_TEN(24), "a250", "a251", "a252", "a253", "a254", "a255");
+}
+#undef ALCS_TEN
+// A register that a vector instruction wrote may be a matrix instruction's operand two states later, a matrix
+// instruction's result may be read 19 states later at the latest.
 __device__ inline void operands_ready() { asm volatile("s_nop 1"); }
-// The last matrix instruction writes its result within 16 passes of four cycles.
-template <int FM, int FN> __device__ inline void matrix_done(v4f (&acc)[FM][FN]) {
-    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) asm volatile("" : "+a"(acc[i][j]));
-}
+__device__ inline void matrix_done() { asm volatile("s_nop 15\n\ts_nop 15"); }
+
+// f(0), ..., f(N - 1), each a constant
+template <class F, int... I> __device__ inline void each_of(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F> __device__ inline void each(F &&f) { each_of(std::make_integer_sequence<int, N>{}, f); }
 
 // ------------------------------------------------------------------------------ what follows the sum
 
@@ -425,10 +448,9 @@ __device__ inline void finish_tile(const Args &a, const v4f (&acc)[FM][FN], int 
     }
 }
 
-// The same for 128 x 128 accumulators, through the wavefront's 32 KB of LDS, 64 rows at a time, so that the gate
-// is a short loop and a row leaves in 16-byte stores: [row][16-byte piece ^ (row & 7)].
-template <class T, bool GATED>
-__device__ inline void finish_big(const Args &a, const v4f (&acc)[8][8], char *mine, int m0, int n0, int result, int lane) {
+// The same for k_big's 128 x 128 accumulators, through 16 KB of LDS of the wavefront's own, 32 rows at a time, so that
+// the gate is a short loop and a row leaves in 16-byte stores: [row][16-byte piece ^ (row & 7)].
+template <class T, bool GATED> __device__ inline void finish_big(const Args &a, char *mine, int m0, int n0, int result, int lane) {
     constexpr bool kExact = sizeof(T) == 4;
     constexpr int kLanes = GATED ? 8 : 16;  // of a row: eight columns (of both projections) a lane
     const int r = lane & 15, q = lane >> 4;
@@ -439,16 +461,14 @@ __device__ inline void finish_big(const Args &a, const v4f (&acc)[8][8], char *m
         b0[e] = a.bias[0] && e < left ? a.bias[0][n + e] : 0.0f;
         b1[e] = GATED && a.bias[1] && e < left ? a.bias[1][n + e] : 0.0f;
     }
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                *(v4f *)(mine + (i * 16 + r) * 512 + (((j * 4 + q) ^ (r & 7)) << 4)) = acc[half * 4 + i][j];
+    each<4>([&](auto quarter) {
+        each<16>([&](auto k) {
+            constexpr int i = decltype(k)::value / 8, j = decltype(k)::value % 8;
+            *(v4f *)(mine + (i * 16 + r) * 512 + (((j * 4 + q) ^ (r & 7)) << 4)) = read_at<(decltype(quarter)::value * 2 + i) * 8 + j>();
+        });
 #pragma clang loop unroll_count(2)
-        for (int it = 0; it < kLanes; ++it) {
-            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + half * 64 + row;
+        for (int it = 0; it < kLanes / 2; ++it) {
+            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + quarter * 32 + row;
             float c[8], u[8], h[8];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -477,22 +497,27 @@ __device__ inline void finish_big(const Args &a, const v4f (&acc)[8][8], char *m
                 store8((T *)a.pre[1] + at, u, left, a.vec);
             }
         }
-    }
+    });
 }
 
 // ------------------------------------------------------------------------------ the kernel
 
-// The tile of a workgroup: workgroups are dealt round-robin to the XCDs, so numbers are exchanged such that
-// an XCD works on neighbouring tiles, columns of up to 8 tiles of rows at a time, and shares their operands in its L2.
-__device__ inline bool tile_of(const Args &a, int &m, int &n, int &z) {
-    const unsigned id = (blockIdx.x % a.xcds) * a.per_xcd + blockIdx.x / a.xcds;
-    if (id >= a.total) return false;
+// Tile number `id` of the result: columns of up to 8 tiles of rows at a time, so that neighbouring numbers share
+// operands.
+__device__ inline void tile_at(const Args &a, unsigned id, int &m, int &n, int &z) {
     const unsigned per = (unsigned)a.tiles_m * a.tiles_n;
     z = (int)(id / per);
     const unsigned t = id % per, strip = t / (8u * a.tiles_n), in = t % (8u * a.tiles_n);
     const unsigned first = strip * 8, rows = min(8u, (unsigned)a.tiles_m - first);
     m = (int)(first + in % rows);
     n = (int)(in / rows);
+}
+// Workgroups are dealt round-robin to the XCDs: numbers are exchanged such that an XCD works on neighbouring tiles and
+// finds their operands in its L2.
+__device__ inline bool tile_of(const Args &a, int &m, int &n, int &z) {
+    const unsigned id = (blockIdx.x % a.xcds) * a.per_xcd + blockIdx.x / a.xcds;
+    if (id >= a.total) return false;
+    tile_at(a, id, m, n, z);
     return true;
 }
 
@@ -664,24 +689,29 @@ template <int E, bool KSTRIDED> struct BigStage {
     }
 };
 
+// A workgroup takes tile after tile: the next one's first K tile is on its way while this one's result leaves.
 template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 1) void k_big(const Args a) {
     constexpr int kA = kBigSide * kTileBytes, kS = E == kMX4 ? kBigSide * 8 : 0, kBuf = 2 * kA + 2 * kS, kK = 8 * per16(E);
+    constexpr int kLoads = 16 + (E == kMX4 ? 4 : 0);  // a wavefront's of a K tile
     extern __shared__ __align__(16) char lds[];
-    int tm, tn, z;
-    if (!tile_of(a, tm, tn, z)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    const int m0 = tm * kBigSide, n0 = tn * (GATED ? kBigSide / 2 : kBigSide);
-    const int result = a.results == 2 ? z : 0;
-    const int all = a.ktiles * a.segs;
+    const int all = a.ktiles * a.segs, kmin = min(a.KA, a.KB);
+    const unsigned first = blockIdx.x % a.xcds * a.per_xcd, end = min(first + a.per_xcd, a.total);
+    unsigned id = first + blockIdx.x / a.xcds;
+    if (id >= end) return;
+    claim_accumulators();
 
-    v4f acc[8][8] = {};
+    int m0, n0, result;
     BigStage<E, AK> sa;
     BigStage<E, BK> sb;
     long long stepA = 0, stepB = 0;
-    int next = 0, in_seg = 0;  // the next tile to send for, and its number in its segment
-    unsigned to = lds_offset(lds);
+    int next = 0, in_seg = 0;  // the K tile to send for next, and its number in its segment
+    const unsigned lds0 = lds_offset(lds);
     auto segment = [&](bool second) {
+        // nothing that depends on this copy of the lane is computed ahead and kept in registers through the loop
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
         const bool sA = second || result == 1;
         const long long pitchA = sA ? a.A[1].pitch : a.A[0].pitch;
         // a gated product's second operand: a wavefront loads rows of one projection
@@ -713,8 +743,17 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
             sb.start_scales(wave, lane, [&](int row) { return min(row, a.N - 1 - n0); }, pitchB);
         }
     };
-    // one sixteenth of the loads of tile `next`
-    auto issue = [&](auto whole, int part) {
+    auto begin = [&](unsigned tile) {
+        int tm, tn, z;
+        tile_at(a, tile, tm, tn, z);
+        m0 = tm * kBigSide;
+        n0 = tn * (GATED ? kBigSide / 2 : kBigSide);
+        result = a.results == 2 ? z : 0;
+        next = in_seg = 0;
+        segment(false);
+    };
+    // one sixteenth of the loads of K tile `next`
+    auto issue = [&](auto whole, int part, unsigned to) {
         constexpr bool kWhole = decltype(whole)::value;
         const int leftA = a.KA - in_seg * kK, leftB = a.KB - in_seg * kK;
         if (part < 8) sa.template issue<kWhole>(part, leftA, to, wave, lane);
@@ -732,90 +771,116 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
             segment(true);
         }
     };
+    auto is_whole = [&] { return (in_seg + 1) * kK <= kmin; };
+    auto issue_all = [&](unsigned to) {
+        if (is_whole()) {
+#pragma unroll
+            for (int part = 0; part < 16; ++part) issue(std::true_type{}, part, to);
+        } else {
+#pragma unroll
+            for (int part = 0; part < 16; ++part) issue(std::false_type{}, part, to);
+        }
+        issued();
+    };
     const Reader<E, kBigSide, AK> ra(wm * 128, lane);
     const Reader<E, kBigSide, BK> rb(wn * 128, lane);
-    const unsigned lds0 = to;
-
-    segment(false);
-#pragma unroll
-    for (int part = 0; part < 16; ++part) issue(std::false_type{}, part);
-    issued();
-    wait_loads();
-    __syncthreads();
-    if (next < all) {
-        to = lds0 + kBuf;
-#pragma unroll
-        for (int part = 0; part < 16; ++part) issue(std::false_type{}, part);
-        issued();
-    }
     v4i pa[8], pb[8], qa[8], qb[8];  // fragments of a first and of a second step
-    int ca[8] = {}, cb[8] = {};      // a tile's scales: step s takes byte s
-    auto scales = [&](const char *here) {
-        if (E != kMX4) return;
-        const int at = ((lane & 15) * 2 + (lane >> 5)) * 16, shift = (lane & 16);
-#pragma unroll
-        for (int f = 0; f < 8; f += 4) {
-            const v4i va = *(const v4i *)(here + 2 * kA + (wm * 8 + f) * 128 + at);
-            const v4i vb = *(const v4i *)(here + 2 * kA + kS + (wn * 8 + f) * 128 + at);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                ca[f + j] = (unsigned)va[j] >> shift;
-                cb[f + j] = (unsigned)vb[j] >> shift;
-            }
-        }
+    // A tile's scales, step s takes byte s: as they lie in LDS, shifted for the first step, and a copy of those for the
+    // second (while it runs, the next tile's come in).
+    v4i raw[4] = {};
+    int ca[8] = {}, cb[8] = {}, da[8] = {}, db[8] = {};
+    const int scale_at = ((lane & 15) * 2 + (lane >> 5)) * 16, shift = lane & 16;
+    auto read_scales = [&](const char *here, int k) {
+        const char *p = here + 2 * kA + scale_at + (k & 1) * 512;
+        raw[k] = *(const v4i *)(k < 2 ? p + wm * 1024 : p + kS + wn * 1024);
     };
-#pragma unroll
-    for (int f = 0; f < 8; ++f) {
-        pa[f] = ra.get(lds, f, 0);
-        pb[f] = rb.get(lds + kA, f, 0);
-    }
-    scales(lds);
+    auto shift_scale = [&](int k) {
+        int &c = k < 8 ? ca[k & 7] : cb[k & 7];
+        asm volatile("v_lshrrev_b32 %0, %1, %2" : "=v"(c) : "v"(shift), "v"(raw[k / 4][k & 3]));
+    };
+    auto copy_scale = [&](int k) {
+        int &d = k < 8 ? da[k & 7] : db[k & 7];
+        asm volatile("v_mov_b32 %0, %1" : "=v"(d) : "v"(k < 8 ? ca[k & 7] : cb[k & 7]));
+    };
     // A wavefront issues in order, and a matrix instruction keeps its unit busy for four issues: one other
     // instruction fits behind each without a gap, several in a row do not.
-    for (int t = 0; t < all; ++t) {
-        char *here = lds + (t & 1) * kBuf, *there = lds + (~t & 1) * kBuf;
+    auto first_step = [&](const char *here) {
         operands_ready();
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int at = i * 8 + j;
-                multiply_in_place<E, 0>(acc[i][j], pb[j], pa[i], cb[j], ca[i]);
-                if (at < 32 && at % 4 == 0) qb[at / 4] = rb.get(here + kA, at / 4, 1);
-                if (at < 32 && at % 4 == 2) qa[at / 4] = ra.get(here, at / 4, 1);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        int da[8], db[8];
-#pragma unroll
-        for (int f = 0; f < 8; ++f) { da[f] = ca[f]; db[f] = cb[f]; }
-        wait_loads();
+        each<64>([&](auto k) {
+            constexpr int at = decltype(k)::value, i = at / 8, j = at % 8;
+            multiply_at<E, 0, at>(pb[j], pa[i], cb[j], ca[i]);
+            if constexpr (at < 32 && at % 4 == 0) qb[at / 4] = rb.get(here + kA, at / 4, 1);
+            if constexpr (at < 32 && at % 4 == 2) qa[at / 4] = ra.get(here, at / 4, 1);
+            if constexpr (E == kMX4 && at >= 40 && at < 56) copy_scale(at - 40);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // (behind the last tile the fragments read are those of an old one, and nobody multiplies them)
+    auto second_step = [&](auto load, const char *there, unsigned to) {
+        operands_ready();
+        each<64>([&](auto k) {
+            constexpr int at = decltype(k)::value, i = at / 8, j = at % 8;
+            multiply_at<E, 1, at>(qb[j], qa[i], db[j], da[i]);
+            if constexpr (at < 32 && at % 4 == 0) pb[at / 4] = rb.get(there + kA, at / 4, 0);
+            if constexpr (at < 32 && at % 4 == 2) pa[at / 4] = ra.get(there, at / 4, 0);
+            if constexpr (decltype(load)::value && at % 4 == 3) issue(std::true_type{}, at / 4, to);
+            if constexpr (E == kMX4 && at >= 32 && at < 36) read_scales(there, at - 32);
+            if constexpr (E == kMX4 && at >= 46 && at < 62) shift_scale(at - 46);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    begin(id);
+    issue_all(lds0);
+    for (;;) {
+        if (next < all) {
+            issue_all(lds0 + kBuf);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"i"(kLoads) : "memory");  // the first K tile's, and everything before
+        } else {
+            wait_loads();
+        }
         __syncthreads();
-        const bool more = next < all, whole = more && (in_seg + 1) * kK <= min(a.KA, a.KB);
-        to = lds0 + (t & 1) * kBuf;
-        if (more && !whole) {
 #pragma unroll
-            for (int part = 0; part < 16; ++part) issue(std::false_type{}, part);
+        for (int f = 0; f < 8; ++f) {
+            pa[f] = ra.get(lds, f, 0);
+            pb[f] = rb.get(lds + kA, f, 0);
         }
-        operands_ready();
-        // (behind the last tile the fragments are those of an old one, and nobody multiplies them)
+        if (E == kMX4) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+            for (int k = 0; k < 4; ++k) read_scales(lds, k);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int at = i * 8 + j;
-                multiply_in_place<E, 1>(acc[i][j], qb[j], qa[i], db[j], da[i]);
-                if (at < 32 && at % 4 == 0) pb[at / 4] = rb.get(there + kA, at / 4, 0);
-                if (at < 32 && at % 4 == 2) pa[at / 4] = ra.get(there, at / 4, 0);
-                if (at % 4 == 3 && whole) issue(std::true_type{}, at / 4);
-                if (at == 40) scales(there);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int k = 0; k < 16; ++k) shift_scale(k);
+        }
+        each<64>([&](auto k) { clear_at<decltype(k)::value>(); });
+        for (int t = 0; t < all; ++t) {
+            char *here = lds + (t & 1) * kBuf, *there = lds + (~t & 1) * kBuf;
+            first_step(here);
+            wait_loads();
+            __syncthreads();
+            const unsigned to = lds0 + (t & 1) * kBuf;
+            if (next < all && is_whole()) {
+                second_step(std::true_type{}, there, to);
+                issued();
+            } else {
+                if (next < all) issue_all(to);
+                second_step(std::false_type{}, there, to);
             }
         }
-        if (more) issued();
+        matrix_done();
+        __syncthreads();  // nobody reads LDS any more
+        const int m = m0 + wm * 128, n = n0 + wn * (GATED ? 64 : 128), which = result;
+        id += gridDim.x / a.xcds;
+        const bool more = id < end;
+        if (more) {
+            begin(id);
+            issue_all(lds0);
+        }
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        finish_big<T, GATED>(a, lds + kBuf + wave * 16384, m, n, which, l);
+        if (!more) break;
+        __syncthreads();
     }
-    matrix_done(acc);
-    __syncthreads();
-    finish_big<T, GATED>(a, acc, lds + wave * 32768, m0 + wm * 128, n0 + wn * (GATED ? 64 : 128), result, lane);
 }
 
 // The sums of a split K, added in the order of the splits; a thread has four neighbours of a row.
@@ -990,12 +1055,13 @@ int launch_one(Args &a, hipStream_t stream) {
     hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(WM * WN * 64), lds, stream, a);
     return launched();
 }
-template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, hipStream_t stream) {
+template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, int cus, hipStream_t stream) {
     constexpr int lds = 4 * (kBigSide * kTileBytes + (E == kMX4 ? kBigSide * 8 : 0));
     auto kern = k_big<E, T, AK, BK, GATED>;
     const int rc = allow_lds((const void *)kern, lds);
     if (rc != ALCS_OK) return rc;
-    hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(256), lds, stream, a);
+    const unsigned share = std::max(1, cus / (int)a.xcds);  // one workgroup per compute unit
+    hipLaunchKernelGGL(kern, dim3(std::min(a.per_xcd, share) * a.xcds), dim3(256), lds, stream, a);
     return launched();
 }
 // The product that `a` describes (operands, sizes, outputs and segs / results set), tiles by `plan`.
@@ -1010,14 +1076,14 @@ int launch_tiles(Args a, const Plan &plan, bool aligned, void *workspace, int cu
     a.per_xcd = (unsigned)((total + xcds - 1) / xcds);
     int rc;
     if constexpr (E == kMX4) {
-        rc = plan.big ? launch_big<E, T, AK, BK, GATED>(a, stream)
+        rc = plan.big ? launch_big<E, T, AK, BK, GATED>(a, cus, stream)
                       : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream);
     } else if constexpr (E == kF32) {
         rc = aligned ? launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream)
                      : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, false>(a, stream);
     } else {
         rc = !aligned ? launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, false>(a, stream)
-             : plan.big ? launch_big<E, T, AK, BK, GATED>(a, stream)
+             : plan.big ? launch_big<E, T, AK, BK, GATED>(a, cus, stream)
                         : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream);
     }
     if (rc != ALCS_OK || a.splits == 1) return rc;
