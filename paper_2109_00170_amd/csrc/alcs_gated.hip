@@ -18,7 +18,6 @@ struct GradArgs {
     int T, F, pitch;     // pitch of dG and dU, elements
     int rows, gate, vec; // rows of a part; vec: G, U, dH may be read four elements at a time
 };
-constexpr int kGradRows = 64;
 
 template <class T> __device__ inline void load4(const T *p, int n, int vec, float v[4]) {
     if (vec && n >= 4) {
@@ -40,23 +39,24 @@ template <class T> __global__ __launch_bounds__(256) void k_gate_grad(const Grad
     float sg[4] = {}, su[4] = {};
     if (c < a.pitch) {
         const int n = a.F - c;
+#pragma clang loop unroll_count(4)
         for (int r = r0 + y; r < r1; r += 4) {
             const long long at = (long long)r * a.F + c;
             float g[4], u[4], h[4], dg[4], du[4];
             load4((const T *)a.G + at, n, a.vec, g);
             load4((const T *)a.U + at, n, a.vec, u);
             load4((const T *)a.dH + at, n, a.vec, h);
+            float v[4], d[4];
+            gate_slopes<sizeof(T) == 4>(a.gate, g, v, d);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float v, d;
-                gate_both<sizeof(T) == 4>(a.gate, g[i], v, d);
-                du[i] = i < n ? h[i] * v : 0.0f;
-                dg[i] = i < n ? h[i] * u[i] * d : 0.0f;
+                du[i] = i < n ? h[i] * v[i] : 0.0f;
+                dg[i] = i < n ? h[i] * u[i] * d[i] : 0.0f;
                 sg[i] += dg[i];
                 su[i] += du[i];
             }
-            store4((T *)a.dG + (long long)r * a.pitch + c, dg, 4, 4);
-            store4((T *)a.dU + (long long)r * a.pitch + c, du, 4, 4);
+            store4((T *)a.dG + (long long)r * a.pitch + c, dg, 4, 1);
+            store4((T *)a.dU + (long long)r * a.pitch + c, du, 4, 1);
         }
     }
     if (!a.sums) return;
@@ -73,12 +73,23 @@ template <class T> __global__ __launch_bounds__(256) void k_gate_grad(const Grad
         a.sums[((long long)blockIdx.y * 2 + plane) * a.F + n] = s;
     }
 }
-// the parts' sums, in their order
+// The parts' sums: 32 columns and eight shares of the parts a workgroup, each added in the order of the parts, the
+// shares in theirs.
 template <class T> __global__ __launch_bounds__(256) void k_bias_grad(const float *sums, int parts, int F, T *dbg, T *dbu) {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= 2LL * F) return;
+    __shared__ float join[8][32];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const long long at = (long long)blockIdx.x * 32 + x;
     float s = 0.0f;
-    for (int k = 0; k < parts; ++k) s += sums[(long long)k * 2 * F + at];
+    if (at < 2LL * F) {
+        const int from = (int)((long long)parts * y / 8), to = (int)((long long)parts * (y + 1) / 8);
+#pragma clang loop unroll_count(8)
+        for (int k = from; k < to; ++k) s += sums[(long long)k * 2 * F + at];
+    }
+    join[y][x] = s;
+    __syncthreads();
+    if (y || at >= 2LL * F) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s += join[k][x];
     T *out = at < F ? dbg : dbu;
     if (out) out[at % F] = (T)s;
 }
@@ -102,12 +113,15 @@ inline bool aligned_rows(const void *p, long long ld, int columns, int E, int ro
     return (uintptr_t)p % 16 == 0 && columns % n == 0 && (ld % n == 0 || rows <= 1);
 }
 
+inline Shape forward_shape(int E, int T, int D, int F) { return {E, true, false, false, T, F, D, 1, 1}; }
+inline Shape dx_shape(int E, int T, int D, int pitch) { return {E, false, false, true, T, D, pitch, 2, 1}; }
+inline Shape dw_shape(int E, int T, int D, int F) { return {E, false, true, true, F, D, T, 1, 2}; }
+
 template <int E> int gated_as(Args a, bool aligned, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     typedef typename TypeOf<E>::type T;
-    if (a.M <= kFewRows) return launch_few<E, T, true>(a, aligned, stream);
+    if (few_rows(a.M, a.N, cus)) return launch_few<E, T, true>(a, aligned, stream);
     const bool near = aligned && near_rows({a.A[0].pitch, a.B[0].pitch, a.B[1].pitch});
-    Plan p = plan_tiles(E, near, true, a.M, a.N, a.KA, 1, 1, cus);
-    if (!workspace || workspace_bytes < p.workspace) { p.splits = 1; p.workspace = 0; }
+    const Plan p = plan_tiles(forward_shape(E, a.M, a.KA, a.N), near, workspace ? workspace_bytes : 0, cus);
     return launch_tiles<E, T, false, false, true>(a, p, aligned, workspace, cus, xcds, stream);
 }
 
@@ -121,14 +135,16 @@ inline BackwardSpace backward_space(int T, int D, int F, int E, int cus) {
     const int n = per16(E);
     s.pitch = (F + n - 1) / n * n;
     const long long each = ((long long)T * s.pitch * bytes_of(E) + 255) / 256 * 256;
-    // parts of 64 rows, longer ones where there are more than 1024
-    s.rows = std::max(kGradRows, (T + 1023) / 1024);
+    // parts of 64 rows, longer ones where there are more than 1024; of 16 (all of a thread's loads in flight at once)
+    // where that makes no more workgroups than the card runs together: 333 x 2730, bfloat16, 5 us, not 23
+    const long long strips = (s.pitch + 255) / 256;
+    s.rows = strips * ((T + 15) / 16) <= 8LL * cus ? 16 : std::max(64, (T + 1023) / 1024);
     s.parts = (T + s.rows - 1) / s.rows;
     s.dG = 0;
     s.dU = each;
     s.sums = 2 * each;
     s.partial = s.sums + ((long long)s.parts * 2 * F * 4 + 255) / 256 * 256;
-    s.total = s.partial + std::max(workspace_of(E, false, T, D, s.pitch, 2, 1, cus), workspace_of(E, false, F, D, T, 1, 2, cus));
+    s.total = s.partial + std::max(workspace_of(dx_shape(E, T, D, s.pitch), cus), workspace_of(dw_shape(E, T, D, F), cus));
     return s;
 }
 
@@ -158,7 +174,7 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
     hipLaunchKernelGGL((k_gate_grad<T>), dim3((unsigned)((s.pitch + 255) / 256), (unsigned)s.parts), dim3(256), 0, stream, g);
     if ((rc = launched()) != ALCS_OK) return rc;
     if (g.sums) {
-        hipLaunchKernelGGL((k_bias_grad<T>), dim3((unsigned)((2LL * b.F + 255) / 256)), dim3(256), 0, stream, g.sums, s.parts, b.F,
+        hipLaunchKernelGGL((k_bias_grad<T>), dim3((unsigned)((2LL * b.F + 31) / 32)), dim3(256), 0, stream, g.sums, s.parts, b.F,
                            (T *)b.dbg, (T *)b.dbu);
         if ((rc = launched()) != ALCS_OK) return rc;
     }
@@ -173,9 +189,9 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         a.segs = 2; a.results = 1;
         a.out[0] = b.dX;
         a.ldo = b.D;
-        a.vec = store_width({b.dX}, b.D, (int)sz);
+        a.vec = rows_of_eights({b.dX}, b.D);
         const bool al = aligned_rows(b.Wg, b.ldg, b.D, E, b.F) && aligned_rows(b.Wu, b.ldu, b.D, E, b.F);
-        const Plan p = plan_tiles(E, al && near_rows({pitch, b.ldg * sz, b.ldu * sz}), false, b.T, b.D, s.pitch, 2, 1, cus);
+        const Plan p = plan_tiles(dx_shape(E, b.T, b.D, s.pitch), al && near_rows({pitch, b.ldg * sz, b.ldu * sz}), INT64_MAX, cus);
         if ((rc = launch_tiles<E, T, false, true, false>(a, p, al, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
     if (b.dWg) {  // dWg = dG^T X and dWu = dU^T X
@@ -187,9 +203,9 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         a.segs = 1; a.results = 2;
         a.out[0] = b.dWg; a.out[1] = b.dWu;
         a.ldo = b.D;
-        a.vec = store_width({b.dWg, b.dWu}, b.D, (int)sz);
+        a.vec = rows_of_eights({b.dWg, b.dWu}, b.D);
         const bool al = aligned_rows(b.X, b.ldx, b.D, E, b.T);
-        const Plan p = plan_tiles(E, al && near_rows({pitch, b.ldx * sz}), false, b.F, b.D, b.T, 1, 2, cus);
+        const Plan p = plan_tiles(dw_shape(E, b.T, b.D, b.F), al && near_rows({pitch, b.ldx * sz}), INT64_MAX, cus);
         if ((rc = launch_tiles<E, T, true, true, false>(a, p, al, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
     return ALCS_OK;
@@ -212,7 +228,7 @@ extern "C" long long alcs_gated_ff_workspace_bytes(int T, int D, int F, int dtyp
     const int rc = check(T, D, F, dtype, 0);
     if (rc != ALCS_OK) return rc;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    return T <= kFewRows ? 0 : workspace_of(dtype, true, T, F, D, 1, 1, cus);
+    return few_rows(T, F, cus) ? 0 : workspace_of(forward_shape(dtype, T, D, F), cus);
 }
 extern "C" long long alcs_gated_ff_backward_workspace_bytes(int T, int D, int F, int dtype) {
     int cus = 0, xcds = 0;
@@ -243,7 +259,7 @@ extern "C" int alcs_gated_ff(const void *X_dev, long long ldx, const void *Wg_de
     a.out[0] = H_dev; a.pre[0] = G_dev; a.pre[1] = U_dev;
     a.ldo = F;
     a.act = gate;
-    a.vec = store_width({H_dev, G_dev, U_dev}, F, (int)sz);
+    a.vec = rows_of_eights({H_dev, G_dev, U_dev}, F);
     const bool al = aligned_rows(X_dev, ldx, D, dtype, T) && aligned_rows(Wg_dev, ldg, D, dtype, F) &&
                     aligned_rows(Wu_dev, ldu, D, dtype, F);
     const hipStream_t st = (hipStream_t)stream;

@@ -86,10 +86,11 @@ inline int check_stored(const void *codes, const void *scales) {
 }
 constexpr int kMaxSize = 1 << 28;
 
+inline Shape linear_shape(int M, int N, int K) { return {kMX4, false, false, false, M, N, K, 1, 1}; }
+
 template <class T> int linear_as(const Args &a, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
-    if (a.M <= kFewRows) return launch_few<kMX4, T, false>(a, true, stream);
-    Plan p = plan_tiles(kMX4, near_rows({a.A[0].pitch}), false, a.M, a.N, a.KA, 1, 1, cus);
-    if (!workspace || workspace_bytes < p.workspace) { p.splits = 1; p.workspace = 0; }
+    if (few_rows(a.M, a.N, cus)) return launch_few<kMX4, T, false>(a, true, stream);
+    const Plan p = plan_tiles(linear_shape(a.M, a.N, a.KA), near_rows({a.A[0].pitch}), workspace ? workspace_bytes : 0, cus);
     return launch_tiles<kMX4, T, false, false, false>(a, p, true, workspace, cus, xcds, stream);
 }
 
@@ -149,7 +150,7 @@ extern "C" long long alcs_mx4_linear_workspace_bytes(int M, int N, int K) {
     if (rc != ALCS_OK) return rc;
     int cus = 0, xcds = 0;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    return M <= kFewRows ? 0 : workspace_of(kMX4, false, M, N, K, 1, 1, cus);
+    return few_rows(M, N, cus) ? 0 : workspace_of(linear_shape(M, N, K), cus);
 }
 
 extern "C" int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scales_dev, const uint8_t *W_codes_dev,
@@ -173,7 +174,7 @@ extern "C" int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scal
     a.out[0] = Y_dev;
     a.ldo = N;
     a.act = activation;
-    a.vec = store_width({Y_dev}, N, dtype == ALCS_F32 ? 4 : 2);
+    a.vec = rows_of_eights({Y_dev}, N);
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == ALCS_F32) return linear_as<float>(a, workspace_dev, workspace_bytes, cus, xcds, st);
     if (dtype == ALCS_BF16) return linear_as<__bf16>(a, workspace_dev, workspace_bytes, cus, xcds, st);

@@ -107,6 +107,21 @@ template <bool EXACT> __device__ inline void gate_both(int gate, float g, float 
         default: v = g; d = 1.0f;
     }
 }
+template <bool EXACT> __device__ inline void gate_slopes(int gate, const float (&g)[4], float (&v)[4], float (&d)[4]) {
+#define ALCS_EACH(kind)                                                        \
+    case kind:                                                                 \
+        _Pragma("unroll") for (int e = 0; e < 4; ++e) gate_both<EXACT>(kind, g[e], v[e], d[e]); \
+        break;
+    switch (gate) {
+        ALCS_EACH(ALCS_GATE_NONE)
+        ALCS_EACH(ALCS_GATE_RELU)
+        ALCS_EACH(ALCS_GATE_SILU)
+        ALCS_EACH(ALCS_GATE_GELU)
+        ALCS_EACH(ALCS_GATE_GELU_TANH)
+        ALCS_EACH(ALCS_GATE_SIGMOID)
+    }
+#undef ALCS_EACH
+}
 __device__ inline float activate(int act, float v) {
     if (act == ALCS_ACT_NONE) return v;
     v = fmaxf(v, 0.0f);
@@ -134,7 +149,7 @@ struct Args {
     void *pre[2];        // gated: G and U where the caller keeps them, or null
     long long ldo;       // elements from one row of out (and pre) to the next
     int act;             // alcs_activation, or alcs_gate for a gated product
-    int vec;             // elements that out and pre may be written at a time: 8, 4 or 1
+    int vec;             // out and pre may be written eight elements at a time
 };
 
 __device__ const v4i g_zeros[4] = {};  // what pieces beyond K read
@@ -151,6 +166,13 @@ __device__ inline void lds_load4(const char *g, unsigned lds) {
 }
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// an address that is the same for all lanes, in scalar registers
+__device__ inline const char *scalar(const char *p) {
+    const uintptr_t v = (uintptr_t)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v), hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
+    return (const char *)((uintptr_t)hi << 32 | lo);
+}
+
 typedef __attribute__((address_space(3))) char lds_char;
 __device__ inline unsigned lds_offset(const char *p) { return (unsigned)(uintptr_t)(lds_char *)(char *)p; }
 
@@ -160,8 +182,10 @@ __device__ inline unsigned lds_offset(const char *p) { return (unsigned)(uintptr
 template <int E, int R, int W, bool KSTRIDED, bool ALIGNED> struct Stage {
     static constexpr int kElems = per16(E), kK = 8 * kElems;
     static constexpr int kBytes = R * kTileBytes, kLoads = kBytes / 1024 / W;
-    static constexpr int kScaleLoads = E == kMX4 ? R * 8 / 256 / W : 0;
-    static_assert(kBytes % (1024 * W) == 0 && (E != kMX4 || R * 8 % (256 * W) == 0), "whole loads per wavefront");
+    // (of few rows two wavefronts load the same: every one has the same number of loads in flight)
+    static constexpr int kScaleWaves = R * 8 / 256 < W ? R * 8 / 256 : W, kScaleLoads = E == kMX4 ? R * 8 / 256 / kScaleWaves : 0;
+    static constexpr int kInFlight = kLoads + kScaleLoads;  // of a wavefront and K tile
+    static_assert(kBytes % (1024 * W) == 0 && (E != kMX4 || R * 8 % (256 * kScaleWaves) == 0), "whole loads per wavefront");
     const char *ptr[kLoads];
     const char *sptr[kScaleLoads ? kScaleLoads : 1];
     int k_of[kLoads];   // first k (K contiguous: of the piece; K strided: the row) inside the tile
@@ -211,7 +235,7 @@ template <int E, int R, int W, bool KSTRIDED, bool ALIGNED> struct Stage {
     template <class F> __device__ void start_scales(int wave, int lane, int k0, F row_of) {
 #pragma unroll
         for (int i = 0; i < kScaleLoads; ++i) {
-            const int d = (wave * kScaleLoads + i) * 64 + lane;
+            const int d = (wave % kScaleWaves * kScaleLoads + i) * 64 + lane;
             sptr[i] = row_of(((d >> 7) * 4 + (d & 3)) * 16 + ((d >> 3) & 15)) + k0 / 32 + ((d >> 2) & 1) * 4;
         }
     }
@@ -234,7 +258,7 @@ template <int E, int R, int W, bool KSTRIDED, bool ALIGNED> struct Stage {
             for (int i = 0; i < kScaleLoads; ++i) {
                 const char *g = sptr[i];
                 if (!whole && k0 + ((lane >> 2) & 1) * 128 >= K) g = (const char *)g_zeros;
-                lds_load4(g, slds + (wave * kScaleLoads + i) * 256);
+                lds_load4(g, slds + (wave % kScaleWaves * kScaleLoads + i) * 256);
                 sptr[i] += 8;
             }
         }
@@ -357,7 +381,7 @@ template <int N, class F> __device__ inline void each(F &&f) { each_of(std::make
 // ------------------------------------------------------------------------------ what follows the sum
 
 template <class T> __device__ inline void store4(T *p, const float v[4], int n, int vec) {
-    if (vec >= 4 && n >= 4) {
+    if (vec && n >= 4) {
         struct alignas(sizeof(T) * 4) Four { T e[4]; } f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f.e[i] = (T)v[i];
@@ -368,17 +392,11 @@ template <class T> __device__ inline void store4(T *p, const float v[4], int n, 
             if (i < n) p[i] = (T)v[i];
     }
 }
-template <class T> __device__ inline void store8(T *p, const float v[8], int n, int vec) {
-    if (vec == 8 && n >= 8) {
-        struct alignas(16) Eight { T e[8]; } f;
+template <class T> __device__ inline void store8(T *p, const float (&v)[8]) {
+    struct alignas(16) Eight { T e[8]; } f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f.e[i] = (T)v[i];
-        *(Eight *)p = f;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = (T)v[i];
-    }
+    for (int i = 0; i < 8; ++i) f.e[i] = (T)v[i];
+    *(Eight *)p = f;
 }
 // four neighbours of a row: bias, activation, rounding (once, to the result's type)
 template <class T> __device__ inline void finish_plain(const Args &a, int result, long long m, int n, v4f c) {
@@ -407,74 +425,55 @@ template <class T> __device__ inline void finish_gated(const Args &a, long long 
     }
 }
 
-// a wavefront's accumulators, rows from m0 and columns (of both projections where GATED) from n0 on
-template <class T, int FM, int FN, bool GATED>
-__device__ inline void finish_tile(const Args &a, const v4f (&acc)[FM][FN], int m0, int n0, int result, int split, int lane) {
-    const int r = lane & 15, q = lane >> 4;
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int m = m0 + i * 16 + r;
-        if (m >= a.M) continue;
-        if (GATED) {
-#pragma unroll
-            for (int j = 0; j < FN / 2; ++j) {
-                const int n = n0 + j * 16 + q * 4;
-                const v4f gv = acc[i][j], uv = acc[i][j + FN / 2];
-                if (a.partial) {
-                    float *p = a.partial + ((long long)split * 2 * a.M + m) * a.N + n;
-                    const float g[4] = {gv[0], gv[1], gv[2], gv[3]}, u[4] = {uv[0], uv[1], uv[2], uv[3]};
-                    if (a.N > n) {
-                        store4(p, g, a.N - n, a.N % 4 == 0 ? 4 : 1);
-                        store4(p + (long long)a.M * a.N, u, a.N - n, a.N % 4 == 0 ? 4 : 1);
-                    }
-                } else {
-                    finish_gated<T>(a, m, n, gv, uv);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int n = n0 + j * 16 + q * 4;
-                const v4f c = acc[i][j];
-                if (a.partial) {
-                    const float v[4] = {c[0], c[1], c[2], c[3]};
-                    if (a.N > n)
-                        store4(a.partial + (((long long)split * a.results + result) * a.M + m) * a.N + n, v, a.N - n, a.N % 4 == 0 ? 4 : 1);
-                } else {
-                    finish_plain<T>(a, result, m, n, c);
-                }
-            }
-        }
-    }
-}
+// A wavefront's sums on their way out.  They lie in LDS, rows of COLS floats (of both projections, one behind the
+// other, where GATED), the 16-byte piece c of a row at c ^ (row & 7): from there a row leaves in stores of
+// neighbouring lanes, whatever its alignment, and the gate is a short loop.  Straight from the accumulators a lane would
+// have four values of each of 64 rows' parts: the epilogue of the 128 x 128 tile of an odd-sized product took longer
+// than the rest of it.
+__device__ inline char *slab_at(char *slab, int pitch, int row, int piece) { return slab + row * pitch + ((piece ^ (row & 7)) << 4); }
 
-// The same for k_big's 128 x 128 accumulators, through 16 KB of LDS of the wavefront's own, 32 rows at a time, so that
-// the gate is a short loop and a row leaves in 16-byte stores: [row][16-byte piece ^ (row & 7)].
-template <class T, bool GATED> __device__ inline void finish_big(const Args &a, char *mine, int m0, int n0, int result, int lane) {
+template <class T, bool GATED, int COLS>
+__device__ inline void finish_rows(const Args &a, char *slab, int rows, int m0, int n0, int result, int split, int lane) {
     constexpr bool kExact = sizeof(T) == 4;
-    constexpr int kLanes = GATED ? 8 : 16;  // of a row: eight columns (of both projections) a lane
-    const int r = lane & 15, q = lane >> 4;
-    const int n = n0 + lane % kLanes * 8, left = a.N - n;
-    float b0[8], b1[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        b0[e] = a.bias[0] && e < left ? a.bias[0][n + e] : 0.0f;
-        b1[e] = GATED && a.bias[1] && e < left ? a.bias[1][n + e] : 0.0f;
-    }
-    each<4>([&](auto quarter) {
-        each<16>([&](auto k) {
-            constexpr int i = decltype(k)::value / 8, j = decltype(k)::value % 8;
-            *(v4f *)(mine + (i * 16 + r) * 512 + (((j * 4 + q) ^ (r & 7)) << 4)) = read_at<(decltype(quarter)::value * 2 + i) * 8 + j>();
-        });
+    constexpr int kOut = GATED ? COLS / 2 : COLS, kPitch = COLS * 4;
+    if (a.partial) {
+        // four neighbours a lane where rows of the sums start at 16-byte addresses
+        constexpr int kLanes = COLS / 4;
+        const int piece = lane % kLanes, plane = GATED && piece >= kLanes / 2;
+        const int n = n0 + piece % (kOut / 4) * 4, left = a.N - n;
+        const long long plane0 = GATED ? split * 2 + plane : (long long)split * a.results + result;
 #pragma clang loop unroll_count(2)
-        for (int it = 0; it < kLanes / 2; ++it) {
-            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + quarter * 32 + row;
+        for (int it = 0; it < rows * kLanes / 64; ++it) {
+            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
+            const v4f v = *(const v4f *)slab_at(slab, kPitch, row, piece);
+            if (m >= a.M || left <= 0) continue;
+            float *p = a.partial + (plane0 * a.M + m) * a.N + n;
+            if (a.N % 4 == 0) *(v4f *)p = v;
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) p[e] = v[e];
+        }
+        return;
+    }
+    if (a.vec) {
+        constexpr int kLanes = kOut / 8;
+        const int n = n0 + lane % kLanes * 8, left = a.N - n;
+        float b0[8], b1[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            b0[e] = a.bias[0] && left > 0 ? a.bias[0][n + e] : 0.0f;
+            b1[e] = GATED && a.bias[1] && left > 0 ? a.bias[1][n + e] : 0.0f;
+        }
+#pragma clang loop unroll_count(2)
+        for (int it = 0; it < rows * kLanes / 64; ++it) {
+            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
             float c[8], u[8], h[8];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int piece = lane % kLanes * 2 + k;
-                const v4f v = *(const v4f *)(mine + row * 512 + ((piece ^ (row & 7)) << 4));
-                const v4f w = GATED ? *(const v4f *)(mine + row * 512 + (((piece + 16) ^ (row & 7)) << 4)) : v;
+                const v4f v = *(const v4f *)slab_at(slab, kPitch, row, piece);
+                const v4f w = GATED ? *(const v4f *)slab_at(slab, kPitch, row, piece + COLS / 8) : v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     c[4 * k + e] = v[e] + b0[4 * k + e];
@@ -491,13 +490,33 @@ template <class T, bool GATED> __device__ inline void finish_big(const Args &a, 
                 for (int e = 0; e < 8; ++e) h[e] = activate(a.act, c[e]);
             }
             if (m >= a.M || left <= 0) continue;
-            store8((T *)a.out[GATED ? 0 : result] + at, h, left, a.vec);
+            store8((T *)a.out[GATED ? 0 : result] + at, h);
             if (GATED && a.pre[0]) {
-                store8((T *)a.pre[0] + at, c, left, a.vec);
-                store8((T *)a.pre[1] + at, u, left, a.vec);
+                store8((T *)a.pre[0] + at, c);
+                store8((T *)a.pre[1] + at, u);
             }
         }
-    });
+        return;
+    }
+    constexpr int kLanes = kOut < 64 ? kOut : 64;
+    for (int first = 0; first < kOut; first += kLanes) {
+        const int c = first + lane % kLanes, n = n0 + c;
+        const bool in = n < a.N;
+        const float b0 = a.bias[0] && in ? a.bias[0][n] : 0.0f, b1 = GATED && a.bias[1] && in ? a.bias[1][n] : 0.0f;
+#pragma clang loop unroll_count(4)
+        for (int it = 0; it < rows * kLanes / 64; ++it) {
+            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
+            const float g = *(const float *)(slab_at(slab, kPitch, row, c / 4) + c % 4 * 4) + b0;
+            const float u = GATED ? *(const float *)(slab_at(slab, kPitch, row, (c + kOut) / 4) + c % 4 * 4) + b1 : 0.0f;
+            const long long at = m * a.ldo + n;
+            if (m >= a.M || !in) continue;
+            ((T *)a.out[GATED ? 0 : result])[at] = (T)(GATED ? gate_value<kExact>(a.act, g) * u : activate(a.act, g));
+            if (GATED && a.pre[0]) {
+                ((T *)a.pre[0])[at] = (T)g;
+                ((T *)a.pre[1])[at] = (T)u;
+            }
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------ the kernel
@@ -521,9 +540,9 @@ __device__ inline bool tile_of(const Args &a, int &m, int &n, int &z) {
     return true;
 }
 
-template <int E, class T, int BM, int BN, int WM, int WN, bool AK, bool BK, bool GATED, bool ALIGNED>
-__global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(const Args a) {
-    constexpr int W = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
+// 128 x 128, four wavefronts, for operands of any alignment (through registers where it is not ALIGNED) and distance.
+template <int E, class T, bool AK, bool BK, bool GATED, bool ALIGNED> __global__ __launch_bounds__(256, 2) void k_tile(const Args a) {
+    constexpr int BM = 128, BN = 128, WM = 2, WN = 2, W = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
     constexpr int kA = BM * kTileBytes, kB = BN * kTileBytes, kS = E == kMX4 ? (BM + BN) * 8 : 0;
     constexpr int kBuf = kA + kB + kS, kK = 8 * per16(E);
     extern __shared__ __align__(16) char lds[];
@@ -596,9 +615,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(const Args a) {
             const int at = ((lane & 15) * 2 + (lane >> 5)) * 16, shift = (lane & 16);
 #pragma unroll
             for (int f = 0; f < FM; f += 4) {
-                const v4i v = *(const v4i *)(here + kA + kB + (wm * FM + f) * 128 + at);
+                const int g = wm * FM + f;
+                const v4i v = *(const v4i *)(here + kA + kB + g / 4 * 512 + at);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sca[f + j] = (unsigned)v[j] >> shift;
+                for (int j = 0; j < (FM < 4 ? FM : 4); ++j) sca[f + j] = (unsigned)(FM == 2 && (g & 2) ? v[2 + j] : v[j]) >> shift;
             }
 #pragma unroll
             for (int f = 0; f < FN; f += 4) {
@@ -622,28 +642,27 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(const Args a) {
         }
     }
 
-    finish_tile<T, FM, FN, GATED>(a, acc, m0 + wm * FM * 16, n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
+    __syncthreads();
+    char *slab = lds + wave * (FM * FN * 1024);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            *(v4f *)slab_at(slab, FN * 64, i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[i][j];
+    finish_rows<T, GATED, FN * 16>(a, slab, FM * 16, m0 + wm * FM * 16, n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
 }
 
-// ------------------------------------------------------------------------------ large tiles
-
-// 256 x 256, four wavefronts with 128 x 128 each, one per SIMD: what LDS has to deliver falls with the
-// wavefront's tile (at 128 x 64 its reads and the arriving tiles take as many cycles as the matrix instructions).
-// With one wavefront a SIMD nothing else fills its waits, so the loop is laid out by hand: a K tile is two
-// steps of 64 matrix instructions, and during each the fragments of the next step are read.  One barrier a
-// tile, in front of its second step: by then every wavefront has read this tile to its end and the next one has
-// arrived, so the one after that can be sent for into this tile's buffer, a whole tile ahead.
-constexpr int kBigSide = 256;
-constexpr long long kBigPitch = 1 << 22;  // rows so far apart at most that a tile's offsets fit 32 bits
-
-// As Stage, with 32-bit offsets from a base that is the same for all lanes.
-template <int E, bool KSTRIDED> struct BigStage {
-    static constexpr int R = kBigSide, W = 4, kElems = per16(E), kK = 8 * kElems, kLoads = R * kTileBytes / 1024 / W;
+// As Stage, for aligned operands whose rows lie at most kNearPitch apart: 32-bit offsets from a base that is the same
+// for all lanes, so that sending for a piece costs one load and no address arithmetic.
+constexpr long long kNearPitch = 1 << 22;
+template <int E, int R, bool KSTRIDED> struct NearStage {
+    static constexpr int W = 4, kElems = per16(E), kK = 8 * kElems;
     typedef Stage<E, R, W, KSTRIDED, true> Places;
+    static constexpr int kLoads = Places::kLoads, kScaleLoads = Places::kScaleLoads, kScaleWaves = Places::kScaleWaves;
     unsigned off[kLoads];
     const char *base;
     const char *sbase;
-    unsigned soff[2];
+    unsigned soff[kScaleLoads ? kScaleLoads : 1];
     template <class F> __device__ void start_rows(int wave, int lane, F row_of, long long pitch) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -662,8 +681,8 @@ template <int E, bool KSTRIDED> struct BigStage {
     }
     template <class F> __device__ void start_scales(int wave, int lane, F row_of, long long pitch) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int d = (wave * 2 + i) * 64 + lane;
+        for (int i = 0; i < kScaleLoads; ++i) {
+            const int d = (wave % kScaleWaves * kScaleLoads + i) * 64 + lane;
             soff[i] = (unsigned)row_of(((d >> 7) * 4 + (d & 3)) * 16 + ((d >> 3) & 15)) * (unsigned)(pitch / 16) + ((d >> 2) & 1) * 4;
         }
     }
@@ -681,37 +700,35 @@ template <int E, bool KSTRIDED> struct BigStage {
     }
     template <bool WHOLE> __device__ void issue_scales(int left, unsigned slds, int wave, int lane) const {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const unsigned at = slds + (wave * 2 + i) * 256;
+        for (int i = 0; i < kScaleLoads; ++i) {
+            const unsigned at = slds + (wave % kScaleWaves * kScaleLoads + i) * 256;
             if (WHOLE) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(soff[i]), "s"(sbase), "s"(at) : "memory");
             else lds_load4(((lane >> 2) & 1) * 128 < left ? sbase + soff[i] : (const char *)g_zeros, at);
         }
     }
 };
 
-// A workgroup takes tile after tile: the next one's first K tile is on its way while this one's result leaves.
-template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 1) void k_big(const Args a) {
-    constexpr int kA = kBigSide * kTileBytes, kS = E == kMX4 ? kBigSide * 8 : 0, kBuf = 2 * kA + 2 * kS, kK = 8 * per16(E);
-    constexpr int kLoads = 16 + (E == kMX4 ? 4 : 0);  // a wavefront's of a K tile
-    extern __shared__ __align__(16) char lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave >> 1, wn = wave & 1;
-    const int all = a.ktiles * a.segs, kmin = min(a.KA, a.KB);
-    const unsigned first = blockIdx.x % a.xcds * a.per_xcd, end = min(first + a.per_xcd, a.total);
-    unsigned id = first + blockIdx.x / a.xcds;
-    if (id >= end) return;
-    claim_accumulators();
-
+// Both operands of a BM x BN tile, brought in by four wavefronts (two by two, as they multiply), K tile after K tile.
+template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
+    static constexpr int kA = BM * kTileBytes, kB = BN * kTileBytes, kSA = E == kMX4 ? BM * 8 : 0, kSB = E == kMX4 ? BN * 8 : 0;
+    static constexpr int kBuf = kA + kB + kSA + kSB, kK = 8 * per16(E);
+    typedef NearStage<E, BM, AK> StageA;
+    typedef NearStage<E, BN, BK> StageB;
+    static constexpr int kParts = StageA::kLoads + StageB::kLoads;                             // pieces of issue()
+    static constexpr int kInFlight = kParts + StageA::kScaleLoads + StageB::kScaleLoads;       // loads of a K tile
+    const Args &a;
+    const int wave, lane;
+    StageA sa;
+    StageB sb;
     int m0, n0, result;
-    BigStage<E, AK> sa;
-    BigStage<E, BK> sb;
-    long long stepA = 0, stepB = 0;
-    int next = 0, in_seg = 0;  // the K tile to send for next, and its number in its segment
-    const unsigned lds0 = lds_offset(lds);
-    auto segment = [&](bool second) {
+    long long stepA, stepB;
+    int next, in_seg;  // the K tile to send for next, counted over the segments, and in its own
+    __device__ Feed(const Args &a_, int wave_, int lane_) : a(a_), wave(wave_), lane(lane_) {}
+
+    __device__ void segment(bool second) {
         // nothing that depends on this copy of the lane is computed ahead and kept in registers through the loop
-        int lane = threadIdx.x & 63;
-        asm volatile("" : "+v"(lane));
+        int l = lane;
+        asm volatile("" : "+v"(l));
         const bool sA = second || result == 1;
         const long long pitchA = sA ? a.A[1].pitch : a.A[0].pitch;
         // a gated product's second operand: a wavefront loads rows of one projection
@@ -719,68 +736,196 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
         const long long pitchB = sB ? a.B[1].pitch : a.B[0].pitch;
         const char *pa = sA ? a.A[1].p : a.A[0].p, *pb = sB ? a.B[1].p : a.B[0].p;
         if (AK) {
-            sa.base = pa + (long long)m0 * bytes_of(E);
+            pa += (long long)m0 * bytes_of(E);
             stepA = pitchA * kK;
-            sa.start_columns(wave, lane, (unsigned)pitchA, a.A[0].rows - m0);
+            sa.start_columns(wave, l, (unsigned)pitchA, a.A[0].rows - m0);
         } else {
-            sa.base = pa + m0 * pitchA;
+            pa += m0 * pitchA;
             stepA = kTileBytes;
-            sa.start_rows(wave, lane, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
+            sa.start_rows(wave, l, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
         }
         if (BK) {
-            sb.base = pb + (long long)n0 * bytes_of(E);
+            pb += (long long)n0 * bytes_of(E);
             stepB = pitchB * kK;
-            sb.start_columns(wave, lane, (unsigned)pitchB, a.B[0].rows - n0);
+            sb.start_columns(wave, l, (unsigned)pitchB, a.B[0].rows - n0);
         } else {
-            sb.base = pb + n0 * pitchB;
+            pb += n0 * pitchB;
             stepB = kTileBytes;
-            sb.start_rows(wave, lane, [&](int row) { return min(GATED ? (row >> 7) * 64 + (row & 63) : row, a.N - 1 - n0); }, pitchB);
+            // a wavefront's columns: half of them of the gate, half of the other projection
+            sb.start_rows(wave, l, [&](int row) { return min(GATED ? row / (BN / 2) * (BN / 4) + row % (BN / 4) : row, a.N - 1 - n0); }, pitchB);
         }
+        sa.base = scalar(pa + in_seg * stepA);
+        sb.base = scalar(pb + in_seg * stepB);
         if (E == kMX4) {
-            sa.sbase = (const char *)a.A[0].scales + m0 * (pitchA / 16);
-            sa.start_scales(wave, lane, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
-            sb.sbase = (const char *)a.B[0].scales + n0 * (pitchB / 16);
-            sb.start_scales(wave, lane, [&](int row) { return min(row, a.N - 1 - n0); }, pitchB);
+            sa.start_scales(wave, l, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
+            sb.start_scales(wave, l, [&](int row) { return min(row, a.N - 1 - n0); }, pitchB);
+            sa.sbase = scalar((const char *)a.A[0].scales + m0 * (pitchA / 16) + in_seg * 8);
+            sb.sbase = scalar((const char *)a.B[0].scales + n0 * (pitchB / 16) + in_seg * 8);
         }
-    };
-    auto begin = [&](unsigned tile) {
-        int tm, tn, z;
-        tile_at(a, tile, tm, tn, z);
-        m0 = tm * kBigSide;
-        n0 = tn * (GATED ? kBigSide / 2 : kBigSide);
-        result = a.results == 2 ? z : 0;
-        next = in_seg = 0;
-        segment(false);
-    };
-    // one sixteenth of the loads of K tile `next`
-    auto issue = [&](auto whole, int part, unsigned to) {
-        constexpr bool kWhole = decltype(whole)::value;
+    }
+    // tile (tm, tn) of result z, from K tile `from` on
+    __device__ void begin(int tm, int tn, int z, int from) {
+        m0 = tm * BM;
+        n0 = tn * (GATED ? BN / 2 : BN);
+        result = z;
+        next = from;
+        const int s = from >= a.ktiles;  // (two segments at most)
+        in_seg = from - s * a.ktiles;
+        segment(s);
+    }
+    // one part of the loads of K tile `next`
+    template <bool WHOLE> __device__ void issue(int part, unsigned to) const {
         const int leftA = a.KA - in_seg * kK, leftB = a.KB - in_seg * kK;
-        if (part < 8) sa.template issue<kWhole>(part, leftA, to, wave, lane);
-        else sb.template issue<kWhole>(part - 8, leftB, to + kA, wave, lane);
-        if (E == kMX4 && part == 7) sa.template issue_scales<kWhole>(leftA, to + 2 * kA, wave, lane);
-        if (E == kMX4 && part == 15) sb.template issue_scales<kWhole>(leftB, to + 2 * kA + kS, wave, lane);
-    };
-    auto issued = [&] {
-        sa.base += stepA;
-        sb.base += stepB;
-        if (E == kMX4) { sa.sbase += 8; sb.sbase += 8; }
+        if (part < StageA::kLoads) sa.template issue<WHOLE>(part, leftA, to, wave, lane);
+        else sb.template issue<WHOLE>(part - StageA::kLoads, leftB, to + kA, wave, lane);
+        if (E == kMX4 && part == StageA::kLoads - 1) sa.template issue_scales<WHOLE>(leftA, to + kA + kB, wave, lane);
+        if (E == kMX4 && part == kParts - 1) sb.template issue_scales<WHOLE>(leftB, to + kA + kB + kSA, wave, lane);
+    }
+    __device__ void issued(int end) {
+        sa.base = scalar(sa.base + stepA);
+        sb.base = scalar(sb.base + stepB);
+        if (E == kMX4) { sa.sbase = scalar(sa.sbase + 8); sb.sbase = scalar(sb.sbase + 8); }
         ++next;
-        if (++in_seg == a.ktiles && next < all) {
+        if (++in_seg == a.ktiles && next < end) {
             in_seg = 0;
             segment(true);
         }
-    };
-    auto is_whole = [&] { return (in_seg + 1) * kK <= kmin; };
-    auto issue_all = [&](unsigned to) {
-        if (is_whole()) {
+    }
+    __device__ bool whole() const { return (in_seg + 1) * kK <= min(a.KA, a.KB); }
+    __device__ void issue_all(unsigned to, int end) {
+        if (whole()) {
 #pragma unroll
-            for (int part = 0; part < 16; ++part) issue(std::true_type{}, part, to);
+            for (int part = 0; part < kParts; ++part) issue<true>(part, to);
         } else {
 #pragma unroll
-            for (int part = 0; part < 16; ++part) issue(std::false_type{}, part, to);
+            for (int part = 0; part < kParts; ++part) issue<false>(part, to);
         }
-        issued();
+        issued(end);
+    }
+};
+
+// ------------------------------------------------------------------------------ small tiles
+
+// BM x 128 (64 or 128 rows), NS K tiles in LDS.  A K tile is two steps; the fragments of the next step are read and the
+// pieces of a later tile sent for between the matrix instructions of this one, so that a wavefront waits for neither.
+// One barrier a tile, in front of its second step, as in k_big.  Two workgroups share a compute unit.
+template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 2) void k_mid(const Args a) {
+    typedef Feed<E, BM, 128, AK, BK, GATED> Feeds;
+    constexpr int FM = BM / 32, FN = 4, kA = Feeds::kA, kB = Feeds::kB, kSA = Feeds::kSA, kBuf = Feeds::kBuf;
+    constexpr int kSlots = FM * FN, kReads = FM + FN;
+    extern __shared__ __align__(16) char lds[];
+    int tm, tn, z;
+    if (!tile_of(a, tm, tn, z)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int result = a.results == 2 ? z & 1 : 0, split = a.results == 2 ? z >> 1 : z;
+    const int all = a.ktiles * a.segs;
+    const int from = (int)((long long)all * split / a.splits), to = (int)((long long)all * (split + 1) / a.splits);
+    const unsigned lds0 = lds_offset(lds);
+    Feeds feed(a, wave, lane);
+    feed.begin(tm, tn, result, from);
+#pragma unroll
+    for (int k = 0; k < NS; ++k)
+        if (from + k < to) feed.issue_all(lds0 + k * kBuf, to);
+    const Reader<E, BM, AK> ra(wm * FM * 16, lane);
+    const Reader<E, 128, BK> rb(wn * FN * 16, lane);
+    v4f acc[FM][FN] = {};
+    v4i fa[2][FM], fb[2][FN];
+    int ca[2][FM] = {}, cb[2][FN] = {};  // scales of this tile, [1]: of the next
+    const int scale_at = ((lane & 15) * 2 + (lane >> 5)) * 16, shift = lane & 16;
+    auto read_scales = [&](const char *here, int into) {
+        if (E != kMX4) return;
+        const char *p = here + kA + kB + scale_at;
+        const v4i va = *(const v4i *)(p + wm * FM / 4 * 512), vb = *(const v4i *)(p + kSA + wn * 512);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) ca[into][j] = (unsigned)(FM == 2 && wm & 1 ? va[(2 + j) & 3] : va[j]) >> shift;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) cb[into][j] = (unsigned)vb[j] >> shift;
+    };
+    // K tile t's loads, while those of the ones behind it may still be on their way
+    auto arrived = [&](int t) {
+        if (NS >= 3 && t + NS - 2 < to) asm volatile("s_waitcnt vmcnt(%0)" ::"i"((NS - 2) * Feeds::kInFlight) : "memory");
+        else wait_loads();
+    };
+    if (from + NS - 1 < to) asm volatile("s_waitcnt vmcnt(%0)" ::"i"((NS - 1) * Feeds::kInFlight) : "memory");
+    else wait_loads();
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < FN; ++f) fb[0][f] = rb.get(lds + kA, f, 0);
+#pragma unroll
+    for (int f = 0; f < FM; ++f) fa[0][f] = ra.get(lds, f, 0);
+    read_scales(lds, 0);
+    for (int t = from, buf = 0; t < to; ++t) {
+        char *here = lds + buf * kBuf;
+        const unsigned free = lds0 + buf * kBuf;
+        buf = buf + 1 == NS ? 0 : buf + 1;
+        char *there = lds + buf * kBuf;
+        bool whole = false;
+        auto step = [&](auto which) {
+            constexpr int S = decltype(which)::value;
+            each<kSlots>([&](auto slot) {
+                constexpr int at = decltype(slot)::value, i = at / FN, j = at % FN;
+                acc[i][j] = multiply<E>(fb[S][j], fa[S][i], acc[i][j], S, E == kMX4 ? cb[0][j] : 0, E == kMX4 ? ca[0][i] : 0);
+                // (behind the last tile the fragments are those of an old one, and nobody multiplies them)
+                char *src = S == 0 ? here : there;
+                if constexpr (at < FN) fb[1 - S][at] = rb.get(src + kA, at, 1 - S);
+                else if constexpr (at < kReads) fa[1 - S][at - FN] = ra.get(src, at - FN, 1 - S);
+                if constexpr (S == 1 && at < Feeds::kParts)
+                    if (whole) feed.template issue<true>(at, free);
+                if constexpr (S == 1 && at == kSlots - 2) read_scales(there, 1);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        step(std::integral_constant<int, 0>{});
+        arrived(t + 1);
+        __syncthreads();  // the next tile is there, and nobody reads this one any more
+        const bool more = feed.next < to;
+        whole = more && feed.whole();
+        if (more && !whole) feed.issue_all(free, to);
+        step(std::integral_constant<int, 1>{});
+        if (whole) feed.issued(to);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) ca[0][j] = ca[1][j];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) cb[0][j] = cb[1][j];
+    }
+    __syncthreads();
+    char *slab = lds + wave * (FM * FN * 1024);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) *(v4f *)slab_at(slab, FN * 64, i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[i][j];
+    finish_rows<T, GATED, FN * 16>(a, slab, FM * 16, feed.m0 + wm * FM * 16, feed.n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
+}
+
+// ------------------------------------------------------------------------------ large tiles
+
+// 256 x 256, four wavefronts with 128 x 128 each, one per SIMD: what LDS has to deliver falls with the
+// wavefront's tile (at 128 x 64 its reads and the arriving tiles take as many cycles as the matrix instructions).
+// With one wavefront a SIMD nothing else fills its waits, so the loop is laid out by hand: a K tile is two
+// steps of 64 matrix instructions, and during each the fragments of the next step are read.  One barrier a
+// tile, in front of its second step: by then every wavefront has read this tile to its end and the next one has
+// arrived, so the one after that can be sent for into this tile's buffer, a whole tile ahead.
+constexpr int kBigSide = 256;
+
+// A workgroup takes tile after tile: the next one's first K tile is on its way while this one's result leaves.
+template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 1) void k_big(const Args a) {
+    typedef Feed<E, kBigSide, kBigSide, AK, BK, GATED> Feeds;
+    constexpr int kA = Feeds::kA, kS = Feeds::kSA, kBuf = Feeds::kBuf;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int all = a.ktiles * a.segs;
+    const unsigned first = blockIdx.x % a.xcds * a.per_xcd, end = min(first + a.per_xcd, a.total);
+    unsigned id = first + blockIdx.x / a.xcds;
+    if (id >= end) return;
+    claim_accumulators();
+    const unsigned lds0 = lds_offset(lds);
+    Feeds feed(a, wave, lane);
+    auto begin = [&](unsigned tile) {
+        int tm, tn, z;
+        tile_at(a, tile, tm, tn, z);
+        feed.begin(tm, tn, a.results == 2 ? z : 0, 0);
     };
     const Reader<E, kBigSide, AK> ra(wm * 128, lane);
     const Reader<E, kBigSide, BK> rb(wn * 128, lane);
@@ -823,7 +968,7 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
             multiply_at<E, 1, at>(qb[j], qa[i], db[j], da[i]);
             if constexpr (at < 32 && at % 4 == 0) pb[at / 4] = rb.get(there + kA, at / 4, 0);
             if constexpr (at < 32 && at % 4 == 2) pa[at / 4] = ra.get(there, at / 4, 0);
-            if constexpr (decltype(load)::value && at % 4 == 3) issue(std::true_type{}, at / 4, to);
+            if constexpr (decltype(load)::value && at % 4 == 3) feed.template issue<true>(at / 4, to);
             if constexpr (E == kMX4 && at >= 32 && at < 36) read_scales(there, at - 32);
             if constexpr (E == kMX4 && at >= 46 && at < 62) shift_scale(at - 46);
             __builtin_amdgcn_sched_barrier(0);
@@ -831,11 +976,11 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
     };
 
     begin(id);
-    issue_all(lds0);
+    feed.issue_all(lds0, all);
     for (;;) {
-        if (next < all) {
-            issue_all(lds0 + kBuf);
-            asm volatile("s_waitcnt vmcnt(%0)" ::"i"(kLoads) : "memory");  // the first K tile's, and everything before
+        if (feed.next < all) {
+            feed.issue_all(lds0 + kBuf, all);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"i"(Feeds::kInFlight) : "memory");  // the first K tile's, and everything before
         } else {
             wait_loads();
         }
@@ -858,26 +1003,39 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
             wait_loads();
             __syncthreads();
             const unsigned to = lds0 + (t & 1) * kBuf;
-            if (next < all && is_whole()) {
+            if (feed.next < all && feed.whole()) {
                 second_step(std::true_type{}, there, to);
-                issued();
+                feed.issued(all);
             } else {
-                if (next < all) issue_all(to);
+                if (feed.next < all) feed.issue_all(to, all);
                 second_step(std::false_type{}, there, to);
             }
         }
         matrix_done();
         __syncthreads();  // nobody reads LDS any more
-        const int m = m0 + wm * 128, n = n0 + wn * (GATED ? 64 : 128), which = result;
+        const int m = feed.m0 + wm * 128, n = feed.n0 + wn * (GATED ? 64 : 128), which = feed.result;
         id += gridDim.x / a.xcds;
         const bool more = id < end;
         if (more) {
             begin(id);
-            issue_all(lds0);
+            feed.issue_all(lds0, all);
         }
+        // 16 KB of LDS of the wavefront's own, 32 rows at a time
         int l = lane;
         asm volatile("" : "+v"(l));
-        finish_big<T, GATED>(a, lds + kBuf + wave * 16384, m, n, which, l);
+        char *slab = lds + kBuf + wave * 16384;
+#pragma clang loop unroll(disable)
+        for (int quarter = 0; quarter < 4; ++quarter) {
+            each<4>([&](auto which_quarter) {  // a register has no number that a loop could count
+                if (quarter != which_quarter) return;
+                each<16>([&](auto k) {
+                    constexpr int i = decltype(k)::value / 8, j = decltype(k)::value % 8;
+                    const int row = i * 16 + (l & 15);
+                    *(v4f *)slab_at(slab, 512, row, j * 4 + (l >> 4)) = read_at<(decltype(which_quarter)::value * 2 + i) * 8 + j>();
+                });
+            });
+            finish_rows<T, GATED, 128>(a, slab, 32, m + quarter * 32, n, which, 0, l);
+        }
         if (!more) break;
         __syncthreads();
     }
@@ -1006,39 +1164,83 @@ __global__ __launch_bounds__(512, 2) void k_few(const Args a) {
 
 // ------------------------------------------------------------------------------ launches
 
-// elements that rows of `columns` packed ones may be written at a time, 0 pointers aside
-inline int store_width(std::initializer_list<const void *> outs, int columns, int size) {
+// whether rows of `columns` packed elements may be written eight at a time (null pointers aside)
+inline int rows_of_eights(std::initializer_list<const void *> outs, int columns) {
     uintptr_t all = 0;
     for (const void *p : outs) all |= (uintptr_t)p;
-    return columns % 8 == 0 && all % 16 == 0 ? 8 : columns % 4 == 0 && all % (4 * size) == 0 ? 4 : 1;
+    return columns % 8 == 0 && all % 16 == 0;
 }
+// Kinds of tiles: 256 x 256 (k_big), 128 x 128 and 64 x 128 (k_mid), two workgroups to a compute unit; and for operands
+// that are not aligned, or lie far apart, 128 x 128 (k_tile).
+enum Kind { kBig = 0, k128 = 1, k64 = 2, kAny = 3 };
 struct Plan {
-    bool big;    // 256 x 256 tiles, eight wavefronts; else 128 x 128, four
-    int tiles_m, tiles_n, ktiles, splits;
+    int kind, tiles_m, tiles_n, ktiles, splits;
     long long workspace;  // bytes of sums that a split needs
 };
-// M rows and N columns (of each projection where gated), `results` of them, K elements in each of `segs` segments.
-// near: the operands are aligned and their rows at most kBigPitch apart.
-inline Plan plan_tiles(int E, bool near, bool gated, long long M, long long N, long long K, int segs, int results, int cus) {
-    auto up = [](long long a, long long b) { return (a + b - 1) / b; };
+struct Shape {
+    int E;
+    bool gated, akstrided, bkstrided;
+    long long M, N, K;  // rows, columns (of each projection where gated), elements of K in a segment
+    int segs, results;
+};
+inline long long up(long long a, long long b) { return (a + b - 1) / b; }
+inline Plan plan_of(const Shape &s, int kind, int splits) {
     Plan p{};
-    p.ktiles = (int)up(K, 8 * per16(E));
-    p.big = near && E != kF32 && up(M, 256) * up(N, gated ? 128 : 256) * results >= cus / 2;
-    const int side = p.big ? 256 : 128;
-    p.tiles_m = (int)up(M, side);
-    p.tiles_n = (int)up(N, gated ? side / 2 : side);
-    p.splits = 1;
-    const long long tiles = (long long)p.tiles_m * p.tiles_n * results, all = (long long)p.ktiles * segs;
-    // two of the small tiles run on a compute unit; a part of K is at least four tiles of it
-    if (!p.big && tiles < cus) p.splits = (int)std::max(1LL, std::min({2LL * cus / tiles, all / 4, 16LL}));
-    p.workspace = p.splits > 1 ? (long long)p.splits * (gated ? 2 : results) * M * N * 4 : 0;
+    p.kind = kind;
+    const int rows = kind == kBig ? 256 : kind == k64 ? 64 : 128, cols = kind == kBig ? 256 : 128;
+    p.ktiles = (int)up(s.K, 8 * per16(s.E));
+    p.tiles_m = (int)up(s.M, rows);
+    p.tiles_n = (int)up(s.N, s.gated ? cols / 2 : cols);
+    p.splits = splits;
+    p.workspace = splits > 1 ? (long long)splits * (s.gated ? 2 : s.results) * s.M * s.N * 4 : 0;
     return p;
 }
-inline long long workspace_of(int E, bool gated, long long M, long long N, long long K, int segs, int results, int cus) {
-    return std::max(plan_tiles(E, true, gated, M, N, K, segs, results, cus).workspace,
-                    plan_tiles(E, false, gated, M, N, K, segs, results, cus).workspace);
+// What a plan takes, in microseconds, as measured on MI355X: a launch with its first loads and its stores, then so much
+// for a K tile of 128 bytes a row, of one workgroup alone on its compute unit and of two.  Small tiles of 16 bits
+// alone: 0.32 and 0.50; where the sum runs over rows (transposing reads) a third more; 256 x 256 tiles run at the
+// card's power limit.  A split costs another launch and the sums' way to memory and back at 4 TB/s.
+//   333 x 1000 -> 2 x 2728 (bfloat16): 128 x 128 tiles 13.7 us, 64 rows 15.0 (258 tiles), 128 x 128 in three parts 22
+//   500 x 512 -> 2 x 1365 (float32): 64 rows 23.7 us, 128 x 128 40.2
+//   512 x 8192 -> 1024 (bfloat16): 64 rows in eight parts 30 us, in one 62, 128 x 128 in eight parts 31, 256 x 256 178
+//   2048 x 4096 -> 2 x 4096 (bfloat16): 256 x 256 107 us, 128 x 128 128
+inline double time_of(const Shape &s, const Plan &p, int cus) {
+    struct Cost { double fixed, alone, two; };
+    static const Cost f32[] = {{}, {6, 1.8, 3.6}, {5, 1.0, 1.85}, {7, 2.0, 4.0}};
+    static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}, {7, 0.9, 1.5}};
+    static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}, {7, 1.1, 2.0}};
+    const Cost &c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[p.kind];
+    const double strided = s.bkstrided && s.E != kF32 && p.kind != kBig ? 1.3 : 1.0;
+    const long long tiles = (long long)p.tiles_m * p.tiles_n * s.results * p.splits;
+    const double depth = (double)(long long)(p.ktiles * s.segs / p.splits);
+    double t;
+    if (p.kind == kBig) {
+        t = c.fixed + (double)up(tiles, cus) * (depth * c.alone + 6);
+    } else {
+        const long long full = tiles / (2 * cus), left = tiles % (2 * cus);
+        t = c.fixed + (double)full * (depth * c.two * strided + 2);
+        if (left) t += left <= cus ? depth * c.alone * strided : depth * c.two * std::max(1.0, strided * 0.85);
+    }
+    return p.splits > 1 ? t + 4 + (double)p.workspace * 2 / 4e6 : t;
 }
-inline bool near_rows(std::initializer_list<long long> pitches) { return std::max(pitches) <= kBigPitch; }
+// near: the operands are aligned and their rows at most kNearPitch apart; workspace: bytes there are for a split.
+inline Plan plan_tiles(const Shape &s, bool near, long long workspace, int cus) {
+    Plan best{};
+    double least = 0;
+    for (int kind = near ? kBig : kAny; kind <= (near ? k64 : kAny); ++kind) {
+        if ((kind == kBig && s.E == kF32) || (kind == k64 && s.akstrided)) continue;
+        for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            const Plan p = plan_of(s, kind, splits);
+            if (splits > 1 && (kind == kBig || p.workspace > workspace || p.ktiles * s.segs < 2 * splits)) break;
+            const double t = time_of(s, p, cus);
+            if (best.tiles_m == 0 || t < least) { best = p; least = t; }
+        }
+    }
+    return best;
+}
+inline long long workspace_of(const Shape &s, int cus) {
+    return std::max(plan_tiles(s, true, INT64_MAX, cus).workspace, plan_tiles(s, false, INT64_MAX, cus).workspace);
+}
+inline bool near_rows(std::initializer_list<long long> pitches) { return std::max(pitches) <= kNearPitch; }
 inline int launched() {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return ALCS_OK;
@@ -1046,13 +1248,21 @@ inline int launched() {
     return ALCS_E_HIP;
 }
 
-template <int E, class T, int BM, int BN, int WM, int WN, bool AK, bool BK, bool GATED, bool ALIGNED>
-int launch_one(Args &a, hipStream_t stream) {
-    constexpr int lds = 2 * ((BM + BN) * kTileBytes + (E == kMX4 ? (BM + BN) * 8 : 0));
-    auto kern = k_tile<E, T, BM, BN, WM, WN, AK, BK, GATED, ALIGNED>;
+template <int E, class T, bool AK, bool BK, bool GATED, bool ALIGNED> int launch_any(Args &a, hipStream_t stream) {
+    constexpr int lds = 2 * (256 * kTileBytes + (E == kMX4 ? 256 * 8 : 0));
+    auto kern = k_tile<E, T, AK, BK, GATED, ALIGNED>;
     const int rc = allow_lds((const void *)kern, lds);
     if (rc != ALCS_OK) return rc;
-    hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(WM * WN * 64), lds, stream, a);
+    hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(256), lds, stream, a);
+    return launched();
+}
+template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> int launch_mid(Args &a, hipStream_t stream) {
+    constexpr int lds = NS * Feed<E, BM, 128, AK, BK, GATED>::kBuf;
+    static_assert(lds <= 80 * 1024, "two workgroups on a compute unit");
+    auto kern = k_mid<E, T, BM, NS, AK, BK, GATED>;
+    const int rc = allow_lds((const void *)kern, lds);
+    if (rc != ALCS_OK) return rc;
+    hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(256), lds, stream, a);
     return launched();
 }
 template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, int cus, hipStream_t stream) {
@@ -1068,30 +1278,33 @@ template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, 
 template <int E, class T, bool AK, bool BK, bool GATED>
 int launch_tiles(Args a, const Plan &plan, bool aligned, void *workspace, int cus, int xcds, hipStream_t stream) {
     a.tiles_m = plan.tiles_m; a.tiles_n = plan.tiles_n; a.ktiles = plan.ktiles; a.splits = plan.splits;
+    if (plan.splits > 1 && !workspace) return ALCS_E_INVALID_ARG;
     a.partial = plan.splits > 1 ? (float *)workspace : nullptr;
     const long long total = (long long)a.tiles_m * a.tiles_n * a.results * a.splits;
     if (total > INT32_MAX - 64) return ALCS_E_UNSUPPORTED;
     a.total = (unsigned)total;
     a.xcds = (unsigned)xcds;
     a.per_xcd = (unsigned)((total + xcds - 1) / xcds);
-    int rc;
-    if constexpr (E == kMX4) {
-        rc = plan.big ? launch_big<E, T, AK, BK, GATED>(a, cus, stream)
-                      : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream);
-    } else if constexpr (E == kF32) {
-        rc = aligned ? launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream)
-                     : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, false>(a, stream);
+    int rc = ALCS_E_UNSUPPORTED;
+    if (plan.kind == kAny) {
+        if constexpr (E == kMX4) rc = launch_any<E, T, AK, BK, GATED, true>(a, stream);
+        else rc = aligned ? launch_any<E, T, AK, BK, GATED, true>(a, stream) : launch_any<E, T, AK, BK, GATED, false>(a, stream);
+    } else if (plan.kind == k128) {
+        rc = launch_mid<E, T, 128, 2, AK, BK, GATED>(a, stream);
+    } else if (plan.kind == k64) {
+        if constexpr (!AK) rc = launch_mid<E, T, 64, 3, AK, BK, GATED>(a, stream);
     } else {
-        rc = !aligned ? launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, false>(a, stream)
-             : plan.big ? launch_big<E, T, AK, BK, GATED>(a, cus, stream)
-                        : launch_one<E, T, 128, 128, 2, 2, AK, BK, GATED, true>(a, stream);
+        if constexpr (E != kF32) rc = launch_big<E, T, AK, BK, GATED>(a, cus, stream);
     }
     if (rc != ALCS_OK || a.splits == 1) return rc;
     const long long quads = (long long)(GATED ? 1 : a.results) * a.M * ((a.N + 3) / 4);
     hipLaunchKernelGGL((k_join<T, GATED>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, a);
     return launched();
 }
-constexpr int kFewRows = 64;
+// Sixteen rows are one fragment: the weights' bytes are all that counts, and k_few reads them straight.  Up to 64 rows
+// it still has the shorter way where its workgroups, of 16 columns each, make one round; beyond, tiles read a row of A
+// for 64 columns at once.  64 x 1000 -> 2 x 2728: 7.4 us, tiles 12; 64 x 2048 -> 2 x 8192: 27.9, tiles 16.3 (bfloat16).
+inline bool few_rows(int M, int N, int cus) { return M <= 16 || (M <= 64 && up(N, 16) <= cus); }
 template <int E, class T, bool GATED, bool ALIGNED> int launch_few_as(const Args &a, hipStream_t stream) {
     const int pieces = (a.KA + 16 * per16(E) - 1) / (16 * per16(E)), W = std::max(1, std::min(8, pieces));
     const int MF = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4, lds = W * (GATED ? 2 : 1) * MF * 1024;
