@@ -531,8 +531,8 @@ typedef enum alcs_dtype {
  *   scales_dev, written completely.  A block that holds an infinity or a NaN gets scale 255 and codes 0.
  * alcs_mx4_dequantize: the values in `dtype` -> Y_dev [rows, cols]; exact but where the type has no such number.
  *
- * Codes are 16-byte, scales 4-byte aligned; cols at most 2^28 (ALCS_E_UNSUPPORTED beyond); rows = 0 is a
- * no-op.  Asynchronous on `stream`, nothing allocated.
+ * Codes are 16-byte, scales 4-byte aligned; cols at most 2^26 and 2^35 stored
+ * elements (ALCS_E_UNSUPPORTED beyond); rows = 0 is a no-op.  Asynchronous on `stream`, nothing allocated.
  */
 int alcs_mx4_quantize(const void *X_dev, long long ldx, long long rows, int cols, int dtype, uint8_t *codes_dev,
                       uint8_t *scales_dev, void *stream);
@@ -551,7 +551,8 @@ int alcs_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *scales_dev, lon
  *   workspace_dev: NULL, or device memory of at least alcs_mx4_linear_workspace_bytes(M, N, K) bytes, 16-byte
  *   aligned, the caller's, overwritten: with it, products of few tiles share K out over more workgroups (a
  *   smaller workspace is not used).  Calls that share one must not overlap.
- *   M = 0 is a no-op; M, N, K at most 2^28 and 2^31 tiles of 128 x 128 (ALCS_E_UNSUPPORTED beyond).
+ *   M = 0 is a no-op; M and N at most 2^26, K at most 2^23, fewer than 2^24 tiles of 64 x 128
+ *   (ALCS_E_UNSUPPORTED beyond).
  *   Asynchronous on `stream`, nothing allocated; equal calls give equal bits.
  */
 long long alcs_mx4_linear_workspace_bytes(int M, int N, int K);
@@ -577,8 +578,10 @@ typedef enum alcs_gate {
  *   halves or the alternate rows of one tensor will do); bg_dev, bu_dev [F] float32 or NULL; H_dev [T, F], fully
  *   overwritten.  G_dev and U_dev [T, F], or both NULL, receive G and U (rounded to `dtype`; H is made from
  *   the unrounded ones) for the gradients.  gate: an alcs_gate value (ALCS_E_INVALID_ARG otherwise).
- *   workspace_dev: as for alcs_mx4_linear, alcs_gated_ff_workspace_bytes(T, D, F, dtype) bytes, or NULL.
- *   T = 0 is a no-op; sizes at most 2^28.  Asynchronous on `stream`, nothing allocated; equal calls give equal
+ *   workspace_dev: as for alcs_mx4_linear, alcs_gated_ff_workspace_bytes(T, D, F, dtype) bytes, or NULL.  It also takes
+ *   copies of operands whose rows do not start at 16-byte addresses (or end there, or lie more than 4 MB apart); without
+ *   room for them such a call of many rows is several times slower.
+ *   T = 0 is a no-op; sizes at most 2^26 (ALCS_E_UNSUPPORTED beyond).  Asynchronous on `stream`, nothing allocated; equal calls give equal
  *   bits, a row's result may differ in its last bits with the number of rows it is computed with.
  *
  * alcs_gated_ff_backward: from dH_dev [T, F], the gradient of a number with respect to H, and the forward's

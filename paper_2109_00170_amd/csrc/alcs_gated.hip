@@ -105,46 +105,128 @@ template <class T> int fill_zero(void *p, long long n, hipStream_t stream) {
 
 // ------------------------------------------------------------------------------ host side
 
-constexpr int kMaxSize = 1 << 28;  // rows, columns: tile and piece numbers stay far inside 31 bits
+constexpr int kMaxSize = 1 << 26;  // rows, columns: numbers of pieces and threads stay inside 32 bits
 
-// Rows that the direct loads take: they start at 16-byte addresses and hold whole 16-byte pieces.
-inline bool aligned_rows(const void *p, long long ld, int columns, int E, int rows) {
+// Rows that the tiles' direct loads take: they start at 16-byte addresses, hold whole 16-byte pieces and lie at most
+// kNearPitch apart.
+inline bool near_rows(const void *p, long long ld, int columns, int E, int rows) {
     const int n = per16(E);
-    return (uintptr_t)p % 16 == 0 && columns % n == 0 && (ld % n == 0 || rows <= 1);
+    return (uintptr_t)p % 16 == 0 && columns % n == 0 && (rows <= 1 || (ld % n == 0 && ld * bytes_of(E) <= kNearPitch));
+}
+inline int whole_pieces(int columns, int E) { return (columns + per16(E) - 1) / per16(E) * per16(E); }
+
+// Copies of up to three matrices whose rows the tiles do not take, padded with zeros to whole pieces: a wavefront a row.
+// 2000 x 999 -> 2 x 2731 (bfloat16) 41 + 9 us, where tiles that read odd rows themselves, through registers,
+// took 69.
+struct AlignArgs {
+    const char *from[3];
+    long long pitch[3];  // bytes
+    char *to[3];
+    int rows[3];
+    int columns, pieces;
+};
+template <class T> __global__ __launch_bounds__(256) void k_align(const AlignArgs a) {
+    constexpr int n = 16 / sizeof(T);
+    const int all = a.rows[0] + a.rows[1] + a.rows[2];
+    for (int at = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6); at < all; at += (int)gridDim.x * 4) {
+        int row = at, i = 0;
+        if (row >= a.rows[0]) { row -= a.rows[0]; i = 1; }
+        if (i == 1 && row >= a.rows[1]) { row -= a.rows[1]; i = 2; }
+        const char *from = (i == 0 ? a.from[0] : i == 1 ? a.from[1] : a.from[2]) + row * (i == 0 ? a.pitch[0] : i == 1 ? a.pitch[1] : a.pitch[2]);
+        char *to = (i == 0 ? a.to[0] : i == 1 ? a.to[1] : a.to[2]) + (long long)row * a.pieces * 16;
+        for (int c = threadIdx.x & 63; c < a.pieces; c += 64) {
+            v4i v = {0, 0, 0, 0};
+            const int left = a.columns - c * n;
+            if (left >= n) {
+                __builtin_memcpy(&v, from + (long long)c * 16, 16);
+            } else {
+                T e[n] = {};
+#pragma unroll
+                for (int j = 0; j < n; ++j)
+                    if (j < left) __builtin_memcpy(&e[j], from + (long long)c * 16 + j * sizeof(T), sizeof(T));
+                __builtin_memcpy(&v, e, 16);
+            }
+            *(v4i *)(to + (long long)c * 16) = v;
+        }
+    }
+}
+// Those of the operands that are not near go to `space` (room for all of them); their pointers and pitches follow.
+template <int E> int align_rows(std::initializer_list<Operand *> operands, std::initializer_list<int> rows, int columns, char *space, hipStream_t stream) {
+    typedef typename TypeOf<E>::type T;
+    AlignArgs g{};
+    g.columns = columns;
+    g.pieces = whole_pieces(columns, E) / per16(E);
+    int n = 0;
+    long long total = 0;
+    const int *r = rows.begin();
+    for (Operand *o : operands) {
+        const int count = *r++;
+        if (near_rows(o->p, o->pitch / bytes_of(E), columns, E, count)) continue;
+        g.from[n] = o->p;
+        g.pitch[n] = o->pitch;
+        g.to[n] = space;
+        g.rows[n++] = count;
+        o->p = space;
+        o->pitch = g.pieces * 16LL;
+        space += whole256((long long)count * g.pieces * 16);
+        total += count;
+    }
+    if (!n) return ALCS_OK;
+    hipLaunchKernelGGL((k_align<T>), dim3((unsigned)std::min((total + 3) / 4, 1LL << 16)), dim3(256), 0, stream, g);
+    return launched();
 }
 
-inline Shape forward_shape(int E, int T, int D, int F) { return {E, true, false, false, T, F, D, 1, 1}; }
-inline Shape dx_shape(int E, int T, int D, int pitch) { return {E, false, false, true, T, D, pitch, 2, 1}; }
-inline Shape dw_shape(int E, int T, int D, int F) { return {E, false, true, true, F, D, T, 1, 2}; }
+inline Shape forward_shape(int E, int T, int D, int F) { return {E, true, false, T, F, D, 1, 1}; }
+inline Shape dx_shape(int E, int T, int D, int pitch) { return {E, false, true, T, D, pitch, 2, 1}; }
+inline Shape dw_shape(int E, int T, int D, int F) { return {E, false, true, F, D, T, 1, 2}; }
+inline long long copy_bytes(int rows, int D, int E) { return whole256((long long)rows * whole_pieces(D, E) * bytes_of(E)); }
+inline long long forward_copies(int E, int T, int D, int F) { return copy_bytes(T, D, E) + 2 * copy_bytes(F, D, E); }
 
-template <int E> int gated_as(Args a, bool aligned, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
+template <int E> int gated_as(Args a, char *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     typedef typename TypeOf<E>::type T;
+    const int D = a.KA;
+    const int n = per16(E);
+    const bool aligned = D % n == 0 && (uintptr_t)a.A[0].p % 16 == 0 && (uintptr_t)a.B[0].p % 16 == 0 && (uintptr_t)a.B[1].p % 16 == 0 &&
+                         a.A[0].pitch % 16 == 0 && a.B[0].pitch % 16 == 0 && a.B[1].pitch % 16 == 0;
     if (few_rows(a.M, a.N, cus)) return launch_few<E, T, true>(a, aligned, stream);
-    const bool near = aligned && near_rows({a.A[0].pitch, a.B[0].pitch, a.B[1].pitch});
-    const Plan p = plan_tiles(forward_shape(E, a.M, a.KA, a.N), near, workspace ? workspace_bytes : 0, cus);
-    return launch_tiles<E, T, false, false, true>(a, p, aligned, workspace, cus, xcds, stream);
+    const long long sz = bytes_of(E);
+    const bool near = near_rows(a.A[0].p, a.A[0].pitch / sz, D, E, a.M) && near_rows(a.B[0].p, a.B[0].pitch / sz, D, E, a.N) &&
+                      near_rows(a.B[1].p, a.B[1].pitch / sz, D, E, a.N);
+    if (!workspace) workspace_bytes = 0;
+    if (!near) {
+        const long long copies = forward_copies(E, a.M, D, a.N);
+        if (workspace_bytes < copies) return launch_few<E, T, true>(a, aligned, stream);
+        const int rc = align_rows<E>({&a.A[0], &a.B[0], &a.B[1]}, {a.M, a.N, a.N}, D, workspace, stream);
+        if (rc != ALCS_OK) return rc;
+        workspace += copies;
+        workspace_bytes -= copies;
+        a.KA = a.KB = whole_pieces(D, E);
+    }
+    const Plan p = plan_tiles(forward_shape(E, a.M, a.KA, a.N), workspace_bytes, cus);
+    return launch_tiles<E, T, false, false, true>(a, p, workspace, cus, xcds, stream);
 }
 
 struct BackwardSpace {  // bytes from the start of the workspace
     int pitch;          // of dG and dU, elements
-    long long dG, dU, sums, partial, total;
+    long long dG, dU, sums, copies, partial, total;
     int parts, rows;
 };
 inline BackwardSpace backward_space(int T, int D, int F, int E, int cus) {
     BackwardSpace s{};
-    const int n = per16(E);
-    s.pitch = (F + n - 1) / n * n;
-    const long long each = ((long long)T * s.pitch * bytes_of(E) + 255) / 256 * 256;
+    s.pitch = whole_pieces(F, E);
+    const long long each = whole256((long long)T * s.pitch * bytes_of(E));
     // parts of 64 rows, longer ones where there are more than 1024; of 16 (all of a thread's loads in flight at once)
-    // where that makes no more workgroups than the card runs together: 333 x 2730, bfloat16, 5 us, not 23
+    // where that makes no more workgroups than the card runs together: 333 x 2730, bfloat16, 7 us, not 23
     const long long strips = (s.pitch + 255) / 256;
     s.rows = strips * ((T + 15) / 16) <= 8LL * cus ? 16 : std::max(64, (T + 1023) / 1024);
     s.parts = (T + s.rows - 1) / s.rows;
     s.dG = 0;
     s.dU = each;
     s.sums = 2 * each;
-    s.partial = s.sums + ((long long)s.parts * 2 * F * 4 + 255) / 256 * 256;
-    s.total = s.partial + std::max(workspace_of(dx_shape(E, T, D, s.pitch), cus), workspace_of(dw_shape(E, T, D, F), cus));
+    s.copies = s.sums + whole256((long long)s.parts * 2 * F * 4);
+    s.partial = s.copies + std::max(2 * copy_bytes(F, D, E), copy_bytes(T, D, E));  // the weights', then X's in their place
+    s.total = s.partial + std::max(plan_tiles(dx_shape(E, T, D, s.pitch), INT64_MAX, cus).workspace,
+                                   plan_tiles(dw_shape(E, T, D, F), INT64_MAX, cus).workspace);
     return s;
 }
 
@@ -179,34 +261,36 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         if ((rc = launched()) != ALCS_OK) return rc;
     }
     const long long sz = bytes_of(E), pitch = s.pitch * sz;
+    const int columns = whole_pieces(b.D, E);
     if (b.dX) {  // dX = dG Wg + dU Wu: one sum over two segments
         Args a{};
         a.A[0] = {(const char *)g.dG, pitch, nullptr, b.T};
         a.A[1] = {(const char *)g.dU, pitch, nullptr, b.T};
-        a.B[0] = {(const char *)b.Wg, b.ldg * sz, nullptr, b.D};
-        a.B[1] = {(const char *)b.Wu, b.ldu * sz, nullptr, b.D};
+        a.B[0] = {(const char *)b.Wg, b.ldg * sz, nullptr, columns};
+        a.B[1] = {(const char *)b.Wu, b.ldu * sz, nullptr, columns};
+        if ((rc = align_rows<E>({&a.B[0], &a.B[1]}, {b.F, b.F}, b.D, workspace + s.copies, stream)) != ALCS_OK) return rc;
         a.M = b.T; a.N = b.D; a.KA = s.pitch; a.KB = b.F;
         a.segs = 2; a.results = 1;
         a.out[0] = b.dX;
         a.ldo = b.D;
         a.vec = rows_of_eights({b.dX}, b.D);
-        const bool al = aligned_rows(b.Wg, b.ldg, b.D, E, b.F) && aligned_rows(b.Wu, b.ldu, b.D, E, b.F);
-        const Plan p = plan_tiles(dx_shape(E, b.T, b.D, s.pitch), al && near_rows({pitch, b.ldg * sz, b.ldu * sz}), INT64_MAX, cus);
-        if ((rc = launch_tiles<E, T, false, true, false>(a, p, al, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
+        const Plan p = plan_tiles(dx_shape(E, b.T, b.D, s.pitch), INT64_MAX, cus);
+        if ((rc = launch_tiles<E, T, false, true, false>(a, p, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
     if (b.dWg) {  // dWg = dG^T X and dWu = dU^T X
         Args a{};
         a.A[0] = {(const char *)g.dG, pitch, nullptr, s.pitch};
         a.A[1] = {(const char *)g.dU, pitch, nullptr, s.pitch};
-        a.B[0] = a.B[1] = {(const char *)b.X, b.ldx * sz, nullptr, b.D};
+        a.B[0] = {(const char *)b.X, b.ldx * sz, nullptr, columns};
+        if ((rc = align_rows<E>({&a.B[0]}, {b.T}, b.D, workspace + s.copies, stream)) != ALCS_OK) return rc;
+        a.B[1] = a.B[0];
         a.M = b.F; a.N = b.D; a.KA = a.KB = b.T;
         a.segs = 1; a.results = 2;
         a.out[0] = b.dWg; a.out[1] = b.dWu;
         a.ldo = b.D;
         a.vec = rows_of_eights({b.dWg, b.dWu}, b.D);
-        const bool al = aligned_rows(b.X, b.ldx, b.D, E, b.T);
-        const Plan p = plan_tiles(dw_shape(E, b.T, b.D, b.F), al && near_rows({pitch, b.ldx * sz}), INT64_MAX, cus);
-        if ((rc = launch_tiles<E, T, true, true, false>(a, p, al, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
+        const Plan p = plan_tiles(dw_shape(E, b.T, b.D, b.F), INT64_MAX, cus);
+        if ((rc = launch_tiles<E, T, true, true, false>(a, p, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
     return ALCS_OK;
 }
@@ -228,7 +312,8 @@ extern "C" long long alcs_gated_ff_workspace_bytes(int T, int D, int F, int dtyp
     const int rc = check(T, D, F, dtype, 0);
     if (rc != ALCS_OK) return rc;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    return few_rows(T, F, cus) ? 0 : workspace_of(forward_shape(dtype, T, D, F), cus);
+    if (few_rows(T, F, cus)) return 0;
+    return (D % per16(dtype) ? forward_copies(dtype, T, D, F) : 0) + plan_tiles(forward_shape(dtype, T, whole_pieces(D, dtype), F), INT64_MAX, cus).workspace;
 }
 extern "C" long long alcs_gated_ff_backward_workspace_bytes(int T, int D, int F, int dtype) {
     int cus = 0, xcds = 0;
@@ -260,12 +345,10 @@ extern "C" int alcs_gated_ff(const void *X_dev, long long ldx, const void *Wg_de
     a.ldo = F;
     a.act = gate;
     a.vec = rows_of_eights({H_dev, G_dev, U_dev}, F);
-    const bool al = aligned_rows(X_dev, ldx, D, dtype, T) && aligned_rows(Wg_dev, ldg, D, dtype, F) &&
-                    aligned_rows(Wu_dev, ldu, D, dtype, F);
     const hipStream_t st = (hipStream_t)stream;
-    if (dtype == ALCS_F32) return gated_as<kF32>(a, al, workspace_dev, workspace_bytes, cus, xcds, st);
-    if (dtype == ALCS_BF16) return gated_as<kBF16>(a, al, workspace_dev, workspace_bytes, cus, xcds, st);
-    return gated_as<kF16>(a, al, workspace_dev, workspace_bytes, cus, xcds, st);
+    if (dtype == ALCS_F32) return gated_as<kF32>(a, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
+    if (dtype == ALCS_BF16) return gated_as<kBF16>(a, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
+    return gated_as<kF16>(a, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
 }
 
 extern "C" int alcs_gated_ff_backward(const void *X_dev, long long ldx, const void *Wg_dev, long long ldg, const void *Wu_dev,

@@ -84,14 +84,14 @@ template <class T> __global__ __launch_bounds__(256) void k_mx4_dequantize(const
 inline int check_stored(const void *codes, const void *scales) {
     return codes && scales && (uintptr_t)codes % 16 == 0 && (uintptr_t)scales % 4 == 0 ? ALCS_OK : ALCS_E_INVALID_ARG;
 }
-constexpr int kMaxSize = 1 << 28;
+constexpr int kMaxSize = 1 << 26;
 
-inline Shape linear_shape(int M, int N, int K) { return {kMX4, false, false, false, M, N, K, 1, 1}; }
+inline Shape linear_shape(int M, int N, int K) { return {kMX4, false, false, M, N, K, 1, 1}; }
 
 template <class T> int linear_as(const Args &a, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     if (few_rows(a.M, a.N, cus)) return launch_few<kMX4, T, false>(a, true, stream);
-    const Plan p = plan_tiles(linear_shape(a.M, a.N, a.KA), near_rows({a.A[0].pitch}), workspace ? workspace_bytes : 0, cus);
-    return launch_tiles<kMX4, T, false, false, false>(a, p, true, workspace, cus, xcds, stream);
+    const Plan p = plan_tiles(linear_shape(a.M, a.N, a.KA), workspace ? workspace_bytes : 0, cus);
+    return launch_tiles<kMX4, T, false, false, false>(a, p, workspace, cus, xcds, stream);
 }
 
 }  // namespace tile
@@ -107,7 +107,7 @@ extern "C" int alcs_mx4_quantize(const void *X_dev, long long ldx, long long row
     if (rows == 0) return ALCS_OK;
     if (!X_dev || check_stored(codes_dev, scales_dev) != ALCS_OK) return ALCS_E_INVALID_ARG;
     const int eights = (cols + 127) / 128 * 16;
-    if (rows > (long long)INT32_MAX * 256 / eights) return ALCS_E_UNSUPPORTED;
+    if (rows > ((1LL << 32) - 512) / eights) return ALCS_E_UNSUPPORTED;  // a launch has less than 2^32 threads
     const dim3 grid((unsigned)((rows * eights + 255) / 256));
     uint32_t *c = (uint32_t *)codes_dev, *s = (uint32_t *)scales_dev;
     const hipStream_t st = (hipStream_t)stream;
@@ -127,7 +127,7 @@ extern "C" int alcs_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *scal
     if (rows == 0) return ALCS_OK;
     if (!Y_dev || check_stored(codes_dev, scales_dev) != ALCS_OK) return ALCS_E_INVALID_ARG;
     const int eights = (cols + 127) / 128 * 16;
-    if (rows > (long long)INT32_MAX * 256 / eights) return ALCS_E_UNSUPPORTED;
+    if (rows > ((1LL << 32) - 512) / eights) return ALCS_E_UNSUPPORTED;  // a launch has less than 2^32 threads
     const dim3 grid((unsigned)((rows * eights + 255) / 256));
     const uint32_t *c = (const uint32_t *)codes_dev;
     const hipStream_t st = (hipStream_t)stream;
@@ -142,7 +142,7 @@ extern "C" int alcs_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *scal
 
 static int check_linear(int M, int N, int K) {
     if (M < 0 || N <= 0 || K <= 0 || K % 128) return ALCS_E_INVALID_ARG;
-    return M > tile::kMaxSize || N > tile::kMaxSize || K > tile::kMaxSize ? ALCS_E_UNSUPPORTED : ALCS_OK;
+    return M > tile::kMaxSize || N > tile::kMaxSize || K / 2 > kNearPitch ? ALCS_E_UNSUPPORTED : ALCS_OK;
 }
 
 extern "C" long long alcs_mx4_linear_workspace_bytes(int M, int N, int K) {
@@ -150,7 +150,7 @@ extern "C" long long alcs_mx4_linear_workspace_bytes(int M, int N, int K) {
     if (rc != ALCS_OK) return rc;
     int cus = 0, xcds = 0;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    return few_rows(M, N, cus) ? 0 : workspace_of(linear_shape(M, N, K), cus);
+    return few_rows(M, N, cus) ? 0 : plan_tiles(linear_shape(M, N, K), INT64_MAX, cus).workspace;
 }
 
 extern "C" int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scales_dev, const uint8_t *W_codes_dev,

@@ -30,7 +30,7 @@
 namespace alcs {
 namespace tile {
 
-enum Elem { kF32 = 0, kBF16 = 1, kF16 = 2, kMX4 = 3 };
+enum Elem { kF32 = ALCS_F32, kBF16 = 1, kF16 = 2, kMX4 = 3 };
 constexpr int bytes_of(int E) { return E == kF32 ? 4 : 2; }                  // not for kMX4
 constexpr int per16(int E) { return E == kF32 ? 4 : E == kMX4 ? 32 : 8; }    // elements in 16 bytes
 constexpr int kTileBytes = 128;                                              // of K, per row
@@ -134,7 +134,7 @@ struct Operand {
     const char *p;         // first row (K contiguous) or first k (K strided)
     long long pitch;       // bytes from one to the next
     const uint8_t *scales; // kMX4: a byte per 16 bytes of p, rows of pitch / 16
-    int rows;              // K strided: elements of a k that may be read (whole pieces where the operand is aligned)
+    int rows;              // K strided: elements of a k that may be read, whole pieces
 };
 struct Args {
     Operand A[2], B[2];  // of the K segments (segs = 2), of the two results (results = 2), or gate and up (B)
@@ -178,24 +178,23 @@ __device__ inline unsigned lds_offset(const char *p) { return (unsigned)(uintptr
 
 // ------------------------------------------------------------------------------ one operand's tile
 
-// R rows (of A, or of B: both projections' for a gated product) and 128 bytes of K, brought in by W wavefronts.
-template <int E, int R, int W, bool KSTRIDED, bool ALIGNED> struct Stage {
-    static constexpr int kElems = per16(E), kK = 8 * kElems;
-    static constexpr int kBytes = R * kTileBytes, kLoads = kBytes / 1024 / W;
-    // (of few rows two wavefronts load the same: every one has the same number of loads in flight)
+// K strided, 16 bits: what the position of a unit of 16 rows is exchanged with.  A transposing LDS read serves half a
+// wavefront at a time, eight k's 32 bytes, which have to lie in different banks; rows of 64 elements (half a turn of the
+// banks) differ in the lowest bit of k already.
+template <int R> __device__ inline int column_swap(int k) { return R >= 128 ? (k & 3) | (k >> 1 & 4) : (k >> 1 & 1) | (k >> 2 & 2); }
+
+// Where the pieces of R rows (of A, or of B: both projections' for a gated product) and 128 bytes of K lie, brought in by
+// four wavefronts.
+template <int E, int R, bool KSTRIDED> struct Places {
+    static constexpr int W = 4, kElems = per16(E), kLoads = R * kTileBytes / 1024 / W;
+    // scales: dwords; of few rows two wavefronts load the same, so that every one has the same number of loads in flight
     static constexpr int kScaleWaves = R * 8 / 256 < W ? R * 8 / 256 : W, kScaleLoads = E == kMX4 ? R * 8 / 256 / kScaleWaves : 0;
-    static constexpr int kInFlight = kLoads + kScaleLoads;  // of a wavefront and K tile
-    static_assert(kBytes % (1024 * W) == 0 && (E != kMX4 || R * 8 % (256 * kScaleWaves) == 0), "whole loads per wavefront");
-    const char *ptr[kLoads];
-    const char *sptr[kScaleLoads ? kScaleLoads : 1];
-    int k_of[kLoads];   // first k (K contiguous: of the piece; K strided: the row) inside the tile
-    int left[kLoads];   // K strided: elements of the piece inside the operand
-    v4i held[ALIGNED ? 1 : kLoads];
+    static_assert(R * kTileBytes % (1024 * W) == 0 && (E != kMX4 || R * 8 % (256 * kScaleWaves) == 0), "whole loads per wavefront");
 
     // K contiguous: the 16 bytes of K that piece c of a row holds.  4-bit: a lane reads pieces c and c + 4, and should
     // find their scales next to each other.
     static __device__ int block_at(int c) { return E == kMX4 ? (c & 3) * 2 + (c >> 2) : c; }
-    // where lane `lane`'s piece of load i lies: row of the tile (K contiguous) or k and first row (K strided)
+    // where lane `lane`'s piece of load i lies: row of the tile and first k (K contiguous), or k and first row (K strided)
     static __device__ void place(int i, int wave, int lane, int &row, int &k) {
         const int o = (wave * kLoads + i) * 1024 + lane * 16;
         if (!KSTRIDED) {
@@ -206,84 +205,8 @@ template <int E, int R, int W, bool KSTRIDED, bool ALIGNED> struct Stage {
             k = o / RB;
             const int piece = (o % RB) / 16;
             if (E == kF32) row = ((piece >> 2) ^ ((k >> 2) & 3)) * 16 + (piece & 3) * 4;
-            else row = ((piece >> 1) ^ ((k & 3) | ((k >> 1) & 4))) * 16 + (piece & 1) * 8;
+            else row = ((piece >> 1) ^ column_swap<R>(k)) * 16 + (piece & 1) * 8;
         }
-    }
-    // K contiguous: row_of(row) = where tile row `row` starts (of a row that exists)
-    template <class F> __device__ void start_rows(int wave, int lane, int k0, F row_of) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            int row;
-            place(i, wave, lane, row, k_of[i]);
-            ptr[i] = row_of(row) + (long long)(k0 + k_of[i]) / kElems * 16;
-        }
-    }
-    // K strided: tile row 0 is element `first` of every k
-    __device__ void start_columns(int wave, int lane, int k0, const char *p, long long pitch, int first, int rows) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            int row;
-            place(i, wave, lane, row, k_of[i]);
-            const int r = first + row, l = rows - r;
-            left[i] = l < 0 ? 0 : l > kElems ? kElems : l;
-            // aligned operands have whole pieces: one beyond them reads the last, for columns that nobody stores
-            ptr[i] = p + (k0 + k_of[i]) * pitch + (long long)(ALIGNED && l < kElems ? rows - kElems : r) * bytes_of(E);
-        }
-    }
-    // row_of(row) = where the scales of tile row `row` start; the tile's scales lie in LDS as dwords (four blocks),
-    // [64 rows][row & 15][half of the tile][16 rows], so that a lane reads those of four fragments at once
-    template <class F> __device__ void start_scales(int wave, int lane, int k0, F row_of) {
-#pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i) {
-            const int d = (wave % kScaleWaves * kScaleLoads + i) * 64 + lane;
-            sptr[i] = row_of(((d >> 7) * 4 + (d & 3)) * 16 + ((d >> 3) & 15)) + k0 / 32 + ((d >> 2) & 1) * 4;
-        }
-    }
-    // the loads of the K tile that starts at k0 (of K) into the LDS region at `lds`; `step` bytes to the next one
-    __device__ void issue(int k0, int K, unsigned lds, unsigned slds, int wave, int lane, long long step) {
-        const bool whole = k0 + kK <= K;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if (ALIGNED) {
-                const char *g = ptr[i];
-                if (!whole && k0 + k_of[i] >= K) g = (const char *)g_zeros;
-                lds_load16(g, lds + (wave * kLoads + i) * 1024);
-            } else {
-                held[i] = fetch(i, k0, K);
-            }
-            ptr[i] += step;
-        }
-        if (E == kMX4) {
-#pragma unroll
-            for (int i = 0; i < kScaleLoads; ++i) {
-                const char *g = sptr[i];
-                if (!whole && k0 + ((lane >> 2) & 1) * 128 >= K) g = (const char *)g_zeros;
-                lds_load4(g, slds + (wave % kScaleWaves * kScaleLoads + i) * 256);
-                sptr[i] += 8;
-            }
-        }
-    }
-    // unaligned operands: through registers, a piece that is not whole element by element
-    __device__ v4i fetch(int i, int k0, int K) const {
-        typedef typename TypeOf<E>::type T;
-        v4i v = {0, 0, 0, 0};
-        int n;
-        if (KSTRIDED) n = k0 + k_of[i] < K ? left[i] : 0;
-        else n = K - (k0 + k_of[i]) < 0 ? 0 : K - (k0 + k_of[i]) > kElems ? kElems : K - (k0 + k_of[i]);
-        if (n == kElems) {
-            __builtin_memcpy(&v, ptr[i], 16);
-        } else {
-            T e[kElems] = {};
-#pragma unroll
-            for (int j = 0; j < kElems; ++j)
-                if (j < n) __builtin_memcpy(&e[j], ptr[i] + j * sizeof(T), sizeof(T));
-            __builtin_memcpy(&v, e, 16);
-        }
-        return v;
-    }
-    __device__ void put(char *lds, int wave, int lane) const {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) *(v4i *)(lds + (wave * kLoads + i) * 1024 + lane * 16) = held[i];
     }
 };
 
@@ -307,7 +230,7 @@ template <int E, int R, bool KSTRIDED> struct Reader {
             return v;
         }
         const int k = s * 32 + q * 8 + (r >> 2);
-        const char *p = lds + k * RB + ((u ^ ((r >> 2) | ((q & 1) << 2))) << 5) + (r & 3) * 8;
+        const char *p = lds + k * RB + ((u ^ column_swap<R>(k)) << 5) + (r & 3) * 8;
         typedef __attribute__((address_space(3))) v4s lds_v4s;
         const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(char *)p);
         const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(char *)(p + 4 * RB));
@@ -519,7 +442,7 @@ __device__ inline void finish_rows(const Args &a, char *slab, int rows, int m0, 
     }
 }
 
-// ------------------------------------------------------------------------------ the kernel
+// ------------------------------------------------------------------------------ tiles and workgroups
 
 // Tile number `id` of the result: columns of up to 8 tiles of rows at a time, so that neighbouring numbers share
 // operands.
@@ -540,125 +463,12 @@ __device__ inline bool tile_of(const Args &a, int &m, int &n, int &z) {
     return true;
 }
 
-// 128 x 128, four wavefronts, for operands of any alignment (through registers where it is not ALIGNED) and distance.
-template <int E, class T, bool AK, bool BK, bool GATED, bool ALIGNED> __global__ __launch_bounds__(256, 2) void k_tile(const Args a) {
-    constexpr int BM = 128, BN = 128, WM = 2, WN = 2, W = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
-    constexpr int kA = BM * kTileBytes, kB = BN * kTileBytes, kS = E == kMX4 ? (BM + BN) * 8 : 0;
-    constexpr int kBuf = kA + kB + kS, kK = 8 * per16(E);
-    extern __shared__ __align__(16) char lds[];
-    int tm, tn, z;
-    if (!tile_of(a, tm, tn, z)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / WN, wn = wave % WN;
-    const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
-    const int result = a.results == 2 ? z & 1 : 0, split = a.results == 2 ? z >> 1 : z;
-    // this split's K tiles, over all segments
-    const int all = a.ktiles * a.segs;
-    const int from = (int)((long long)all * split / a.splits), to = (int)((long long)all * (split + 1) / a.splits);
-
-    v4f acc[FM][FN] = {};
-    Stage<E, BM, W, AK, ALIGNED> sa;
-    Stage<E, BN, W, BK, ALIGNED> sb;
-    int seg = -1;
-    long long stepA = 0, stepB = 0;
-    auto issue = [&](int t, int buf) {
-        const int s = t / a.ktiles, k0 = (t - s * a.ktiles) * kK;
-        if (s != seg) {  // the first tile, or the first of the next segment
-            seg = s;
-            const bool second = a.segs == 2 ? s == 1 : result == 1;
-            const char *pa = second ? a.A[1].p : a.A[0].p, *pb = a.segs == 2 && s == 1 ? a.B[1].p : a.B[0].p;
-            const long long pitchA = second ? a.A[1].pitch : a.A[0].pitch;
-            const long long pitchB = a.segs == 2 && s == 1 ? a.B[1].pitch : a.B[0].pitch;
-            stepA = AK ? pitchA * kK : kTileBytes;
-            stepB = BK ? pitchB * kK : kTileBytes;
-            if (AK) sa.start_columns(wave, lane, k0, pa, pitchA, m0, a.A[0].rows);
-            else sa.start_rows(wave, lane, k0, [&](int row) { return pa + min(m0 + row, a.M - 1) * pitchA; });
-            if (BK) sb.start_columns(wave, lane, k0, pb, pitchB, n0, a.B[0].rows);
-            else if (GATED) sb.start_rows(wave, lane, k0, [&](int row) {
-                // a wavefront's columns: half of them of the gate, half of the other projection
-                constexpr int half = BN / WN / 2;
-                const int w = row / (2 * half), j = row % (2 * half), n = min(n0 + w * half + j % half, a.N - 1);
-                return j < half ? a.B[0].p + n * a.B[0].pitch : a.B[1].p + n * a.B[1].pitch;
-            });
-            else sb.start_rows(wave, lane, k0, [&](int row) { return pb + min(n0 + row, a.N - 1) * pitchB; });
-            if (E == kMX4) {
-                sa.start_scales(wave, lane, k0, [&](int row) {
-                    return (const char *)a.A[0].scales + min(m0 + row, a.M - 1) * (pitchA / 16);
-                });
-                sb.start_scales(wave, lane, k0, [&](int row) {
-                    return (const char *)a.B[0].scales + min(n0 + row, a.N - 1) * (pitchB / 16);
-                });
-            }
-        }
-        const unsigned at = lds_offset(lds) + buf * kBuf;
-        sa.issue(k0, a.KA, at, at + kA + kB, wave, lane, stepA);
-        sb.issue(k0, a.KB, at + kA, at + kA + kB + BM * 8, wave, lane, stepB);
-    };
-    const Reader<E, BM, AK> ra(wm * FM * 16, lane);
-    const Reader<E, BN, BK> rb(wn * FN * 16, lane);
-
-    if (from < to) issue(from, 0);
-    for (int t = from; t < to; ++t) {
-        const int buf = (t - from) & 1;
-        char *here = lds + buf * kBuf;
-        if (!ALIGNED) {
-            sa.put(here, wave, lane);
-            sb.put(here + kA, wave, lane);
-        }
-        wait_loads();
-        __syncthreads();  // this tile is there, and nobody reads the other buffer any more
-        if (t + 1 < to) issue(t + 1, buf ^ 1);
-        int sca[FM], scb[FN];
-        if (E == kMX4) {
-            // a lane's two blocks of a tile are 2q and 2q + 1: a dword of four fragments' at a time, shifted so
-            // that step s takes byte s
-            const int at = ((lane & 15) * 2 + (lane >> 5)) * 16, shift = (lane & 16);
-#pragma unroll
-            for (int f = 0; f < FM; f += 4) {
-                const int g = wm * FM + f;
-                const v4i v = *(const v4i *)(here + kA + kB + g / 4 * 512 + at);
-#pragma unroll
-                for (int j = 0; j < (FM < 4 ? FM : 4); ++j) sca[f + j] = (unsigned)(FM == 2 && (g & 2) ? v[2 + j] : v[j]) >> shift;
-            }
-#pragma unroll
-            for (int f = 0; f < FN; f += 4) {
-                const v4i v = *(const v4i *)(here + kA + kB + BM * 8 + (wn * FN + f) * 128 + at);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) scb[f + j] = (unsigned)v[j] >> shift;
-            }
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            v4i fa[FM], fb[FN];
-#pragma unroll
-            for (int f = 0; f < FN; ++f) fb[f] = rb.get(here + kA, f, s);
-#pragma unroll
-            for (int f = 0; f < FM; ++f) fa[f] = ra.get(here, f, s);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    acc[i][j] = multiply<E>(fb[j], fa[i], acc[i][j], s, E == kMX4 ? scb[j] : 0, E == kMX4 ? sca[i] : 0);
-        }
-    }
-
-    __syncthreads();
-    char *slab = lds + wave * (FM * FN * 1024);
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-            *(v4f *)slab_at(slab, FN * 64, i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[i][j];
-    finish_rows<T, GATED, FN * 16>(a, slab, FM * 16, m0 + wm * FM * 16, n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
-}
-
-// As Stage, for aligned operands whose rows lie at most kNearPitch apart: 32-bit offsets from a base that is the same
-// for all lanes, so that sending for a piece costs one load and no address arithmetic.
+// One operand on its way: aligned, rows at most kNearPitch apart, so that a piece has a 32-bit offset from a base that is
+// the same for all lanes and sending for it costs one load and no address arithmetic.
 constexpr long long kNearPitch = 1 << 22;
 template <int E, int R, bool KSTRIDED> struct NearStage {
-    static constexpr int W = 4, kElems = per16(E), kK = 8 * kElems;
-    typedef Stage<E, R, W, KSTRIDED, true> Places;
-    static constexpr int kLoads = Places::kLoads, kScaleLoads = Places::kScaleLoads, kScaleWaves = Places::kScaleWaves;
+    typedef Places<E, R, KSTRIDED> At;
+    static constexpr int kElems = At::kElems, kK = 8 * kElems, kLoads = At::kLoads, kScaleLoads = At::kScaleLoads, kScaleWaves = At::kScaleWaves;
     unsigned off[kLoads];
     const char *base;
     const char *sbase;
@@ -667,7 +477,7 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             int row, k;
-            Places::place(i, wave, lane, row, k);
+            At::place(i, wave, lane, row, k);
             off[i] = (unsigned)row_of(row) * (unsigned)pitch + k / kElems * 16;
         }
     }
@@ -675,7 +485,7 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             int row, k;
-            Places::place(i, wave, lane, row, k);
+            At::place(i, wave, lane, row, k);
             off[i] = k * pitch + (unsigned)min(row, left - kElems) * bytes_of(E);
         }
     }
@@ -694,7 +504,7 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
         } else {
             int row, k, l = lane;
             asm volatile("" : "+v"(l));  // the last tile's business: nothing of it is kept in registers by the loop
-            Places::place(i, wave, l, row, k);
+            At::place(i, wave, l, row, k);
             lds_load16(k < left ? base + off[i] : (const char *)g_zeros, at);
         }
     }
@@ -1066,8 +876,8 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void k_join(con
 
 // ------------------------------------------------------------------------------ few rows
 
-// Up to 16 * MF rows of A (a token, a few requests): the weights are read once and the product is bound by
-// their bytes, so nothing is staged.  A workgroup has 16 columns (of both projections where GATED); its wavefronts
+// 16 * MF rows of A (a token, a few requests) a workgroup: the weights are read once and the product is bound by
+// their bytes, so nothing is staged.  Operands of any alignment and distance.  A workgroup has 16 columns (of both projections where GATED); its wavefronts
 // share out K in pieces of 256 bytes a row, read their fragments straight from memory, four steps ahead of
 // the multiply, and add their sums through LDS in a fixed order.  Rows of A beyond M read the last row.
 template <int E, bool ALIGNED> __device__ inline v4i piece_of(const char *row, int k, int K) {
@@ -1096,7 +906,8 @@ __global__ __launch_bounds__(512, 2) void k_few(const Args a) {
     constexpr int kElems = per16(E), P = GATED ? 2 : 1;
     extern __shared__ __align__(16) char lds[];  // [wavefront][plane][MF][64] v4f
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6;
-    const int r = lane & 15, q = lane >> 4, n0 = blockIdx.x * 16;
+    const unsigned across = (unsigned)(a.N + 15) / 16;
+    const int r = lane & 15, q = lane >> 4, n0 = (int)(blockIdx.x % across) * 16, m0 = (int)(blockIdx.x / across) * 16 * MF;
     const int n = min(n0 + r, a.N - 1);
     const char *w[P];
 #pragma unroll
@@ -1105,7 +916,7 @@ __global__ __launch_bounds__(512, 2) void k_few(const Args a) {
     const char *xs[MF], *ws = nullptr;
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
-        const int m = min(f * 16 + r, a.M - 1);
+        const int m = min(m0 + f * 16 + r, a.M - 1);
         x[f] = a.A[0].p + m * a.A[0].pitch;
         if (E == kMX4) xs[f] = (const char *)a.A[0].scales + m * (a.A[0].pitch / 16);
     }
@@ -1154,7 +965,7 @@ __global__ __launch_bounds__(512, 2) void k_few(const Args a) {
         for (int k = 0; k < W; ++k)
 #pragma unroll
             for (int p = 0; p < P; ++p) s[p] += ((const v4f *)lds)[((size_t)k * P * MF + p * MF + f) * 64 + lane];
-        const int m = f * 16 + r;
+        const int m = m0 + f * 16 + r;
         if (m < a.M) {
             if (GATED) finish_gated<T>(a, m, n0 + q * 4, s[0], s[P - 1]);
             else finish_plain<T>(a, 0, m, n0 + q * 4, s[0]);
@@ -1170,16 +981,15 @@ inline int rows_of_eights(std::initializer_list<const void *> outs, int columns)
     for (const void *p : outs) all |= (uintptr_t)p;
     return columns % 8 == 0 && all % 16 == 0;
 }
-// Kinds of tiles: 256 x 256 (k_big), 128 x 128 and 64 x 128 (k_mid), two workgroups to a compute unit; and for operands
-// that are not aligned, or lie far apart, 128 x 128 (k_tile).
-enum Kind { kBig = 0, k128 = 1, k64 = 2, kAny = 3 };
+// Kinds of tiles: 256 x 256 (k_big), 128 x 128 and 64 x 128 (k_mid).
+enum Kind { kBig = 0, k128 = 1, k64 = 2 };
 struct Plan {
     int kind, tiles_m, tiles_n, ktiles, splits;
     long long workspace;  // bytes of sums that a split needs
 };
 struct Shape {
     int E;
-    bool gated, akstrided, bkstrided;
+    bool gated, strided;  // strided: the sum runs over the rows of B, or of both
     long long M, N, K;  // rows, columns (of each projection where gated), elements of K in a segment
     int segs, results;
 };
@@ -1205,11 +1015,11 @@ inline Plan plan_of(const Shape &s, int kind, int splits) {
 //   2048 x 4096 -> 2 x 4096 (bfloat16): 256 x 256 107 us, 128 x 128 128
 inline double time_of(const Shape &s, const Plan &p, int cus) {
     struct Cost { double fixed, alone, two; };
-    static const Cost f32[] = {{}, {6, 1.8, 3.6}, {5, 1.0, 1.85}, {7, 2.0, 4.0}};
-    static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}, {7, 0.9, 1.5}};
-    static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}, {7, 1.1, 2.0}};
+    static const Cost f32[] = {{}, {6, 1.8, 3.6}, {5, 1.0, 1.85}};
+    static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}};
+    static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}};
     const Cost &c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[p.kind];
-    const double strided = s.bkstrided && s.E != kF32 && p.kind != kBig ? 1.3 : 1.0;
+    const double strided = s.strided && s.E != kF32 && p.kind != kBig ? 1.3 : 1.0;
     const long long tiles = (long long)p.tiles_m * p.tiles_n * s.results * p.splits;
     const double depth = (double)(long long)(p.ktiles * s.segs / p.splits);
     double t;
@@ -1222,12 +1032,12 @@ inline double time_of(const Shape &s, const Plan &p, int cus) {
     }
     return p.splits > 1 ? t + 4 + (double)p.workspace * 2 / 4e6 : t;
 }
-// near: the operands are aligned and their rows at most kNearPitch apart; workspace: bytes there are for a split.
-inline Plan plan_tiles(const Shape &s, bool near, long long workspace, int cus) {
+// workspace: bytes there are for a split.
+inline Plan plan_tiles(const Shape &s, long long workspace, int cus) {
     Plan best{};
     double least = 0;
-    for (int kind = near ? kBig : kAny; kind <= (near ? k64 : kAny); ++kind) {
-        if ((kind == kBig && s.E == kF32) || (kind == k64 && s.akstrided)) continue;
+    for (int kind : {kBig, k128, k64}) {
+        if (kind == kBig && s.E == kF32) continue;
         for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
             const Plan p = plan_of(s, kind, splits);
             if (splits > 1 && (kind == kBig || p.workspace > workspace || p.ktiles * s.segs < 2 * splits)) break;
@@ -1237,10 +1047,7 @@ inline Plan plan_tiles(const Shape &s, bool near, long long workspace, int cus) 
     }
     return best;
 }
-inline long long workspace_of(const Shape &s, int cus) {
-    return std::max(plan_tiles(s, true, INT64_MAX, cus).workspace, plan_tiles(s, false, INT64_MAX, cus).workspace);
-}
-inline bool near_rows(std::initializer_list<long long> pitches) { return std::max(pitches) <= kNearPitch; }
+inline long long whole256(long long bytes) { return (bytes + 255) / 256 * 256; }
 inline int launched() {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return ALCS_OK;
@@ -1248,14 +1055,6 @@ inline int launched() {
     return ALCS_E_HIP;
 }
 
-template <int E, class T, bool AK, bool BK, bool GATED, bool ALIGNED> int launch_any(Args &a, hipStream_t stream) {
-    constexpr int lds = 2 * (256 * kTileBytes + (E == kMX4 ? 256 * 8 : 0));
-    auto kern = k_tile<E, T, AK, BK, GATED, ALIGNED>;
-    const int rc = allow_lds((const void *)kern, lds);
-    if (rc != ALCS_OK) return rc;
-    hipLaunchKernelGGL(kern, dim3(a.per_xcd * a.xcds), dim3(256), lds, stream, a);
-    return launched();
-}
 template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> int launch_mid(Args &a, hipStream_t stream) {
     constexpr int lds = NS * Feed<E, BM, 128, AK, BK, GATED>::kBuf;
     static_assert(lds <= 80 * 1024, "two workgroups on a compute unit");
@@ -1274,25 +1073,22 @@ template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, 
     hipLaunchKernelGGL(kern, dim3(std::min(a.per_xcd, share) * a.xcds), dim3(256), lds, stream, a);
     return launched();
 }
-// The product that `a` describes (operands, sizes, outputs and segs / results set), tiles by `plan`.
+// The product that `a` describes (operands, sizes, outputs and segs / results set; rows aligned and near), by `plan`.
 template <int E, class T, bool AK, bool BK, bool GATED>
-int launch_tiles(Args a, const Plan &plan, bool aligned, void *workspace, int cus, int xcds, hipStream_t stream) {
+int launch_tiles(Args a, const Plan &plan, void *workspace, int cus, int xcds, hipStream_t stream) {
     a.tiles_m = plan.tiles_m; a.tiles_n = plan.tiles_n; a.ktiles = plan.ktiles; a.splits = plan.splits;
     if (plan.splits > 1 && !workspace) return ALCS_E_INVALID_ARG;
     a.partial = plan.splits > 1 ? (float *)workspace : nullptr;
     const long long total = (long long)a.tiles_m * a.tiles_n * a.results * a.splits;
-    if (total > INT32_MAX - 64) return ALCS_E_UNSUPPORTED;
+    if (total >= (1 << 24) - 64) return ALCS_E_UNSUPPORTED;  // a launch has less than 2^32 threads
     a.total = (unsigned)total;
     a.xcds = (unsigned)xcds;
     a.per_xcd = (unsigned)((total + xcds - 1) / xcds);
     int rc = ALCS_E_UNSUPPORTED;
-    if (plan.kind == kAny) {
-        if constexpr (E == kMX4) rc = launch_any<E, T, AK, BK, GATED, true>(a, stream);
-        else rc = aligned ? launch_any<E, T, AK, BK, GATED, true>(a, stream) : launch_any<E, T, AK, BK, GATED, false>(a, stream);
-    } else if (plan.kind == k128) {
+    if (plan.kind == k128) {
         rc = launch_mid<E, T, 128, 2, AK, BK, GATED>(a, stream);
     } else if (plan.kind == k64) {
-        if constexpr (!AK) rc = launch_mid<E, T, 64, 3, AK, BK, GATED>(a, stream);
+        rc = launch_mid<E, T, 64, 3, AK, BK, GATED>(a, stream);
     } else {
         if constexpr (E != kF32) rc = launch_big<E, T, AK, BK, GATED>(a, cus, stream);
     }
@@ -1301,17 +1097,20 @@ int launch_tiles(Args a, const Plan &plan, bool aligned, void *workspace, int cu
     hipLaunchKernelGGL((k_join<T, GATED>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, a);
     return launched();
 }
-// Sixteen rows are one fragment: the weights' bytes are all that counts, and k_few reads them straight.  Up to 64 rows
-// it still has the shorter way where its workgroups, of 16 columns each, make one round; beyond, tiles read a row of A
-// for 64 columns at once.  64 x 1000 -> 2 x 2728: 7.4 us, tiles 12; 64 x 2048 -> 2 x 8192: 27.9, tiles 16.3 (bfloat16).
-inline bool few_rows(int M, int N, int cus) { return M <= 16 || (M <= 64 && up(N, 16) <= cus); }
+// A few rows of A: k_few's way is the shortest where its workgroups, of 16 columns each, are few; with more, tiles of 64
+// rows stream the weights faster, however few the rows are.  1 x 2048 -> 2 x 8192 (bfloat16): 13.5 us, tiles 15.2;
+// 1 x 4096 -> 2 x 16384: 47 us, tiles 43 (6.3 TB/s); 64 x 1000 -> 2 x 2728: 7.4, tiles 12; 64 x 2048 -> 2 x 8192: 28,
+// tiles 15.3; 1 x 8192 -> 16384 (4-bit): 20.5, tiles 17.3.
+inline bool few_rows(int M, int N, int cus) { return M <= 64 && up(N, 16) <= (M <= 16 ? 2 : 1) * cus; }
 template <int E, class T, bool GATED, bool ALIGNED> int launch_few_as(const Args &a, hipStream_t stream) {
     const int pieces = (a.KA + 16 * per16(E) - 1) / (16 * per16(E)), W = std::max(1, std::min(8, pieces));
     const int MF = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4, lds = W * (GATED ? 2 : 1) * MF * 1024;
     auto kern = MF == 1 ? k_few<E, T, 1, GATED, ALIGNED> : MF == 2 ? k_few<E, T, 2, GATED, ALIGNED> : k_few<E, T, 4, GATED, ALIGNED>;
     const int rc = allow_lds((const void *)kern, lds);
     if (rc != ALCS_OK) return rc;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + 15) / 16)), dim3(W * 64), lds, stream, a);
+    const long long blocks = up(a.N, 16) * up(a.M, 16 * MF);
+    if (blocks >= 1 << 23) return ALCS_E_UNSUPPORTED;  // a launch has less than 2^32 threads
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(W * 64), lds, stream, a);
     return launched();
 }
 template <int E, class T, bool GATED> int launch_few(const Args &a, bool aligned, hipStream_t stream) {
