@@ -31,7 +31,8 @@ template <class T> __device__ inline void load4(const T *p, int n, int vec, floa
     }
 }
 
-template <class T> __global__ __launch_bounds__(256) void k_gate_grad(const GradArgs a) {
+// AHEAD: a thread's rows whose loads are in flight together.
+template <class T, int AHEAD> __global__ __launch_bounds__(256) void k_gate_grad(const GradArgs a) {
     __shared__ float join[4][64][8];
     const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
     const int c = (blockIdx.x * 64 + x) * 4;
@@ -39,7 +40,7 @@ template <class T> __global__ __launch_bounds__(256) void k_gate_grad(const Grad
     float sg[4] = {}, su[4] = {};
     if (c < a.pitch) {
         const int n = a.F - c;
-#pragma clang loop unroll_count(4)
+#pragma clang loop unroll_count(AHEAD)
         for (int r = r0 + y; r < r1; r += 4) {
             const long long at = (long long)r * a.F + c;
             float g[4], u[4], h[4], dg[4], du[4];
@@ -253,7 +254,9 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
     g.T = b.T; g.F = b.F; g.pitch = s.pitch; g.rows = s.rows; g.gate = b.gate;
     const uintptr_t where = (uintptr_t)b.G | (uintptr_t)b.U | (uintptr_t)b.dH;
     g.vec = b.F % 4 == 0 && where % (4 * sizeof(T)) == 0;
-    hipLaunchKernelGGL((k_gate_grad<T>), dim3((unsigned)((s.pitch + 255) / 256), (unsigned)s.parts), dim3(256), 0, stream, g);
+    // (many parts have wavefronts enough: 8192 x 8192, bfloat16, 123 us with one row ahead, 154 with four)
+    auto grad = s.rows == 16 ? k_gate_grad<T, 4> : k_gate_grad<T, 1>;
+    hipLaunchKernelGGL(grad, dim3((unsigned)((s.pitch + 255) / 256), (unsigned)s.parts), dim3(256), 0, stream, g);
     if ((rc = launched()) != ALCS_OK) return rc;
     if (g.sums) {
         hipLaunchKernelGGL((k_bias_grad<T>), dim3((unsigned)((2LL * b.F + 31) / 32)), dim3(256), 0, stream, g.sums, s.parts, b.F,

@@ -469,8 +469,9 @@ constexpr long long kNearPitch = 1 << 22;
 template <int E, int R, bool KSTRIDED> struct NearStage {
     typedef Places<E, R, KSTRIDED> At;
     static constexpr int kElems = At::kElems, kK = 8 * kElems, kLoads = At::kLoads, kScaleLoads = At::kScaleLoads, kScaleWaves = At::kScaleWaves;
+    static constexpr int kBias = 3 * 1024;
     unsigned off[kLoads];
-    const char *base;
+    const char *base;  // kBias in front of the tile's first element
     const char *sbase;
     unsigned soff[kScaleLoads ? kScaleLoads : 1];
     template <class F> __device__ void start_rows(int wave, int lane, F row_of, long long pitch) {
@@ -478,7 +479,7 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
         for (int i = 0; i < kLoads; ++i) {
             int row, k;
             At::place(i, wave, lane, row, k);
-            off[i] = (unsigned)row_of(row) * (unsigned)pitch + k / kElems * 16;
+            off[i] = (unsigned)row_of(row) * (unsigned)pitch + k / kElems * 16 + kBias - i % 4 * 1024;
         }
     }
     __device__ void start_columns(int wave, int lane, unsigned pitch, int left) {  // left: columns from the tile's first on
@@ -486,7 +487,7 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
         for (int i = 0; i < kLoads; ++i) {
             int row, k;
             At::place(i, wave, lane, row, k);
-            off[i] = k * pitch + (unsigned)min(row, left - kElems) * bytes_of(E);
+            off[i] = k * pitch + (unsigned)min(row, left - kElems) * bytes_of(E) + kBias - i % 4 * 1024;
         }
     }
     template <class F> __device__ void start_scales(int wave, int lane, F row_of, long long pitch) {
@@ -496,16 +497,20 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
             soff[i] = (unsigned)row_of(((d >> 7) * 4 + (d & 3)) * 16 + ((d >> 3) & 15)) * (unsigned)(pitch / 16) + ((d >> 2) & 1) * 4;
         }
     }
-    // load i of the K tile; WHOLE: all of it inside K, else `left` elements are
+    // load i of the K tile; WHOLE: all of it inside K, else `left` elements are.  An instruction's own offset moves both its
+    // ends, so every fourth load sets the place in LDS (m0) for four, and off[] is relative to `base` - kBias.
     template <bool WHOLE> __device__ void issue(int i, int left, unsigned lds, int wave, int lane) const {
-        const unsigned at = lds + (wave * kLoads + i) * 1024;
+        const unsigned at = lds + (wave * kLoads + i / 4 * 4) * 1024;
         if (WHOLE) {
-            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]), "s"(base), "s"(at) : "memory");
+            if (i % 4 == 0) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]), "s"(base), "s"(at) : "memory");
+            else if (i % 4 == 1) asm volatile("global_load_lds_dwordx4 %0, %1 offset:1024" ::"v"(off[i]), "s"(base) : "memory");
+            else if (i % 4 == 2) asm volatile("global_load_lds_dwordx4 %0, %1 offset:2048" ::"v"(off[i]), "s"(base) : "memory");
+            else asm volatile("global_load_lds_dwordx4 %0, %1 offset:3072" ::"v"(off[i]), "s"(base) : "memory");
         } else {
             int row, k, l = lane;
             asm volatile("" : "+v"(l));  // the last tile's business: nothing of it is kept in registers by the loop
             At::place(i, wave, l, row, k);
-            lds_load16(k < left ? base + off[i] : (const char *)g_zeros, at);
+            lds_load16(k < left ? base + off[i] + i % 4 * 1024 : (const char *)g_zeros, at + i % 4 * 1024);
         }
     }
     template <bool WHOLE> __device__ void issue_scales(int left, unsigned slds, int wave, int lane) const {
@@ -564,8 +569,8 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
             // a wavefront's columns: half of them of the gate, half of the other projection
             sb.start_rows(wave, l, [&](int row) { return min(GATED ? row / (BN / 2) * (BN / 4) + row % (BN / 4) : row, a.N - 1 - n0); }, pitchB);
         }
-        sa.base = scalar(pa + in_seg * stepA);
-        sb.base = scalar(pb + in_seg * stepB);
+        sa.base = scalar(pa + in_seg * stepA - StageA::kBias);
+        sb.base = scalar(pb + in_seg * stepB - StageB::kBias);
         if (E == kMX4) {
             sa.start_scales(wave, l, [&](int row) { return min(row, a.M - 1 - m0); }, pitchA);
             sb.start_scales(wave, l, [&](int row) { return min(row, a.N - 1 - n0); }, pitchB);
@@ -588,8 +593,11 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
         const int leftA = a.KA - in_seg * kK, leftB = a.KB - in_seg * kK;
         if (part < StageA::kLoads) sa.template issue<WHOLE>(part, leftA, to, wave, lane);
         else sb.template issue<WHOLE>(part - StageA::kLoads, leftB, to + kA, wave, lane);
-        if (E == kMX4 && part == StageA::kLoads - 1) sa.template issue_scales<WHOLE>(leftA, to + kA + kB, wave, lane);
-        if (E == kMX4 && part == kParts - 1) sb.template issue_scales<WHOLE>(leftB, to + kA + kB + kSA, wave, lane);
+    }
+    template <bool WHOLE> __device__ void issue_scales(bool of_b, unsigned to) const {
+        if (E != kMX4) return;
+        if (of_b) sb.template issue_scales<WHOLE>(a.KB - in_seg * kK, to + kA + kB + kSA, wave, lane);
+        else sa.template issue_scales<WHOLE>(a.KA - in_seg * kK, to + kA + kB, wave, lane);
     }
     __device__ void issued(int end) {
         sa.base = scalar(sa.base + stepA);
@@ -606,9 +614,13 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
         if (whole()) {
 #pragma unroll
             for (int part = 0; part < kParts; ++part) issue<true>(part, to);
+            issue_scales<true>(false, to);
+            issue_scales<true>(true, to);
         } else {
 #pragma unroll
             for (int part = 0; part < kParts; ++part) issue<false>(part, to);
+            issue_scales<false>(false, to);
+            issue_scales<false>(true, to);
         }
         issued(end);
     }
@@ -681,7 +693,13 @@ template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global
                 if constexpr (at < FN) fb[1 - S][at] = rb.get(src + kA, at, 1 - S);
                 else if constexpr (at < kReads) fa[1 - S][at - FN] = ra.get(src, at - FN, 1 - S);
                 if constexpr (S == 1 && at < Feeds::kParts)
-                    if (whole) feed.template issue<true>(at, free);
+                    if (whole) {
+                        feed.template issue<true>(at, free);
+                        if (at == Feeds::kParts - 1) {
+                            feed.template issue_scales<true>(false, free);
+                            feed.template issue_scales<true>(true, free);
+                        }
+                    }
                 if constexpr (S == 1 && at == kSlots - 2) read_scales(there, 1);
                 __builtin_amdgcn_sched_barrier(0);
             });
@@ -778,7 +796,10 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
             multiply_at<E, 1, at>(qb[j], qa[i], db[j], da[i]);
             if constexpr (at < 32 && at % 4 == 0) pb[at / 4] = rb.get(there + kA, at / 4, 0);
             if constexpr (at < 32 && at % 4 == 2) pa[at / 4] = ra.get(there, at / 4, 0);
-            if constexpr (decltype(load)::value && at % 4 == 3) feed.template issue<true>(at / 4, to);
+            // (early, but for transposing reads, which are twice as many: spread over the step, dX 3 % faster)
+            constexpr int every = AK || BK ? 4 : 2;
+            if constexpr (decltype(load)::value && at % every == every - 1 && at / every < 16) feed.template issue<true>(at / every, to);
+            if constexpr (decltype(load)::value && (at == 37 || at == 41)) feed.template issue_scales<true>(at == 41, to);
             if constexpr (E == kMX4 && at >= 32 && at < 36) read_scales(there, at - 32);
             if constexpr (E == kMX4 && at >= 46 && at < 62) shift_scale(at - 46);
             __builtin_amdgcn_sched_barrier(0);
