@@ -508,9 +508,10 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
             else asm volatile("global_load_lds_dwordx4 %0, %1 offset:3072" ::"v"(off[i]), "s"(base) : "memory");
         } else {
             int row, k, l = lane;
-            asm volatile("" : "+v"(l));  // the last tile's business: nothing of it is kept in registers by the loop
+            unsigned o = off[i];
+            asm volatile("" : "+v"(l), "+v"(o));  // the last tile's business: nothing of it is kept in registers by the loop
             At::place(i, wave, l, row, k);
-            lds_load16(k < left ? base + off[i] + i % 4 * 1024 : (const char *)g_zeros, at + i % 4 * 1024);
+            lds_load16(k < left ? base + o + i % 4 * 1024 : (const char *)g_zeros, at + i % 4 * 1024);
         }
     }
     template <bool WHOLE> __device__ void issue_scales(int left, unsigned slds, int wave, int lane) const {
@@ -527,6 +528,7 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
 template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
     static constexpr int kA = BM * kTileBytes, kB = BN * kTileBytes, kSA = E == kMX4 ? BM * 8 : 0, kSB = E == kMX4 ? BN * 8 : 0;
     static constexpr int kBuf = kA + kB + kSA + kSB, kK = 8 * per16(E);
+    static constexpr bool kTwo = !AK && BK;  // K in two segments: dX alone
     typedef NearStage<E, BM, AK> StageA;
     typedef NearStage<E, BN, BK> StageB;
     static constexpr int kParts = StageA::kLoads + StageB::kLoads;                             // pieces of issue()
@@ -584,7 +586,7 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
         n0 = tn * (GATED ? BN / 2 : BN);
         result = z;
         next = from;
-        const int s = from >= a.ktiles;  // (two segments at most)
+        const int s = kTwo && from >= a.ktiles;
         in_seg = from - s * a.ktiles;
         segment(s);
     }
@@ -604,9 +606,12 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
         sb.base = scalar(sb.base + stepB);
         if (E == kMX4) { sa.sbase = scalar(sa.sbase + 8); sb.sbase = scalar(sb.sbase + 8); }
         ++next;
-        if (++in_seg == a.ktiles && next < end) {
-            in_seg = 0;
-            segment(true);
+        ++in_seg;
+        if constexpr (kTwo) {
+            if (in_seg == a.ktiles && next < end) {
+                in_seg = 0;
+                segment(true);
+            }
         }
     }
     __device__ bool whole() const { return (in_seg + 1) * kK <= min(a.KA, a.KB); }
@@ -776,12 +781,14 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
         asm volatile("v_mov_b32 %0, %1" : "=v"(d) : "v"(k < 8 ? ca[k & 7] : cb[k & 7]));
     };
     // A wavefront issues in order, and a matrix instruction keeps its unit busy for four issues: one other
-    // instruction fits behind each without a gap, several in a row do not.
+    // instruction fits behind each without a gap, several in a row do not.  Neighbouring instructions share an
+    // operand, also from one row of fragments to the next (the columns go to and fro): fewer registers change.
+    bool ready = false;  // a K tile is left to send for, and all of it lies inside K
     auto first_step = [&](const char *here) {
         operands_ready();
         each<64>([&](auto k) {
-            constexpr int at = decltype(k)::value, i = at / 8, j = at % 8;
-            multiply_at<E, 0, at>(pb[j], pa[i], cb[j], ca[i]);
+            constexpr int at = decltype(k)::value, i = at / 8, j = i % 2 ? 7 - at % 8 : at % 8;
+            multiply_at<E, 0, i * 8 + j>(pb[j], pa[i], cb[j], ca[i]);
             if constexpr (at < 32 && at % 4 == 0) qb[at / 4] = rb.get(here + kA, at / 4, 1);
             if constexpr (at < 32 && at % 4 == 2) qa[at / 4] = ra.get(here, at / 4, 1);
             if constexpr (E == kMX4 && at >= 40 && at < 56) copy_scale(at - 40);
@@ -792,14 +799,18 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
     auto second_step = [&](auto load, const char *there, unsigned to) {
         operands_ready();
         each<64>([&](auto k) {
-            constexpr int at = decltype(k)::value, i = at / 8, j = at % 8;
-            multiply_at<E, 1, at>(qb[j], qa[i], db[j], da[i]);
+            constexpr int at = decltype(k)::value, i = at / 8, j = i % 2 ? 7 - at % 8 : at % 8;
+            multiply_at<E, 1, i * 8 + j>(qb[j], qa[i], db[j], da[i]);
             if constexpr (at < 32 && at % 4 == 0) pb[at / 4] = rb.get(there + kA, at / 4, 0);
             if constexpr (at < 32 && at % 4 == 2) pa[at / 4] = ra.get(there, at / 4, 0);
-            // (early, but for transposing reads, which are twice as many: spread over the step, dX 3 % faster)
+            // (early, but for transposing reads, which are twice as many: spread over the step)
             constexpr int every = AK || BK ? 4 : 2;
-            if constexpr (decltype(load)::value && at % every == every - 1 && at / every < 16) feed.template issue<true>(at / every, to);
-            if constexpr (decltype(load)::value && (at == 37 || at == 41)) feed.template issue_scales<true>(at == 41, to);
+            if constexpr (decltype(load)::value) {
+                if constexpr (at % every == every - 1 && at / every < 16) feed.template issue<true>(at / every, to);
+                if constexpr (at == 37 || at == 41) feed.template issue_scales<true>(at == 41, to);
+                if constexpr (at == (every == 4 ? 63 : 54)) feed.issued(all);
+                if constexpr (at == (every == 4 ? 63 : 58)) ready = feed.next < all && feed.whole();
+            }
             if constexpr (E == kMX4 && at >= 32 && at < 36) read_scales(there, at - 32);
             if constexpr (E == kMX4 && at >= 46 && at < 62) shift_scale(at - 46);
             __builtin_amdgcn_sched_barrier(0);
@@ -828,17 +839,18 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
             for (int k = 0; k < 16; ++k) shift_scale(k);
         }
         each<64>([&](auto k) { clear_at<decltype(k)::value>(); });
+        ready = feed.next < all && feed.whole();
         for (int t = 0; t < all; ++t) {
             char *here = lds + (t & 1) * kBuf, *there = lds + (~t & 1) * kBuf;
             first_step(here);
             wait_loads();
             __syncthreads();
             const unsigned to = lds0 + (t & 1) * kBuf;
-            if (feed.next < all && feed.whole()) {
+            if (ready) {
                 second_step(std::true_type{}, there, to);
-                feed.issued(all);
             } else {
                 if (feed.next < all) feed.issue_all(to, all);
+                ready = feed.next < all && feed.whole();
                 second_step(std::false_type{}, there, to);
             }
         }
