@@ -531,8 +531,8 @@ typedef enum alcs_dtype {
  *   scales_dev, written completely.  A block that holds an infinity or a NaN gets scale 255 and codes 0.
  * alcs_mx4_dequantize: the values in `dtype` -> Y_dev [rows, cols]; exact but where the type has no such number.
  *
- * Codes are 16-byte, scales 4-byte aligned; cols at most 2^26 and 2^35 stored
- * elements (ALCS_E_UNSUPPORTED beyond); rows = 0 is a no-op.  Asynchronous on `stream`, nothing allocated.
+ * Codes are 16-byte, scales 4-byte aligned; cols at most 2^26 and fewer than 2^34
+ * stored elements (ALCS_E_UNSUPPORTED beyond); rows = 0 is a no-op.  Asynchronous on `stream`, nothing allocated.
  */
 int alcs_mx4_quantize(const void *X_dev, long long ldx, long long rows, int cols, int dtype, uint8_t *codes_dev,
                       uint8_t *scales_dev, void *stream);

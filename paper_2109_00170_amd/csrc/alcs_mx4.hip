@@ -25,10 +25,10 @@ template <class T> __device__ inline void load8(const T *p, int n, float v[8]) {
 
 template <class T> __global__ __launch_bounds__(256) void k_mx4_quantize(const T *X, long long ldx, long long rows, int cols,
                                                                         int eights, uint32_t *codes, uint32_t *scales) {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;  // eights (per row) is a multiple of 16
-    if (at >= rows * eights) return;                                 // whole groups of 16 threads leave
-    const long long row = at / eights;
-    const int c = (int)(at % eights) * 8;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x;  // eights (per row) is a multiple of 16
+    if (at >= rows * eights) return;                     // whole groups of 16 threads leave
+    const unsigned row = at / (unsigned)eights;
+    const int c = (int)(at % (unsigned)eights) * 8;
     float v[8];
     load8(X + row * ldx + c, cols - c, v);
     uint32_t top = 0;
@@ -52,31 +52,36 @@ template <class T> __global__ __launch_bounds__(256) void k_mx4_quantize(const T
     if ((threadIdx.x & 15) == 0) scales[at / 16] = byte;
 }
 
-template <class T> __global__ __launch_bounds__(256) void k_mx4_dequantize(const uint32_t *codes, const uint8_t *scales, long long rows,
-                                                                          int cols, int eights, T *Y) {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= rows * eights) return;
-    const long long row = at / eights;
-    const int c = (int)(at % eights) * 8, n = cols - c;
+// A thread has 16 bytes of the result (4 or 8 columns), so that a wavefront's stores are one run.  Bound by the stores.
+template <class T> __global__ __launch_bounds__(256) void k_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, long long rows,
+                                                                          int cols, int pieces, T *Y) {
+    constexpr int kN = 16 / sizeof(T);  // pieces: of a row's stored columns
+    const unsigned at = blockIdx.x * 256 + threadIdx.x;
+    if (at >= rows * pieces) return;
+    const unsigned row = at / (unsigned)pieces;
+    const int c = (int)(at % (unsigned)pieces) * kN, n = cols - c;
     if (n <= 0) return;
-    const uint32_t code = codes[at], scale = scales[at / 4];
-    // value = grid * 2^(scale - 127), in two factors so that neither leaves the range of normal numbers
-    const float a = __uint_as_float((scale / 2 + 64) << 23), b = __uint_as_float((scale - scale / 2 + 63) << 23);
-    const float nan = __uint_as_float(0x7fc00000u);
-    T out[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t k = code >> (4 * i) & 15, m = k & 7;
-        // 0, 0.5, then 1.m0 * 2^(m/2 - 1)
-        const float g = m < 2 ? 0.5f * (float)m : __uint_as_float((126u + m / 2) << 23 | (m & 1) << 22);
-        const float w = (k & 8 ? -g : g) * a * b;
-        out[i] = (T)(scale == 255 ? nan : w);
+    const uint32_t code = kN == 8 ? ((const uint32_t *)codes)[at] : ((const uint16_t *)codes)[at], scale = scales[at / (32 / kN)];
+    const float unit = __uint_as_float(scale ? scale << 23 : 1u << 22), nan = __uint_as_float(0x7fc00000u);
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    v2f w[4];
+    w[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 0);
+    w[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 1);
+    if (kN == 8) {
+        w[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 2);
+        w[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, unit, 3);
     }
-    T *p = Y + row * cols + c;
-    if (n >= 8) __builtin_memcpy(p, out, sizeof(out));
-    else {
+    T out[kN];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kN; ++i) out[i] = (T)(scale == 255 ? nan : w[i / 2][i % 2]);
+    T *p = Y + (long long)row * cols + c;
+    if (n >= kN) {
+        v4i v;
+        __builtin_memcpy(&v, out, 16);
+        __builtin_memcpy(p, &v, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
             if (i < n) p[i] = out[i];
     }
 }
@@ -126,17 +131,16 @@ extern "C" int alcs_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *scal
     if (cols > tile::kMaxSize) return ALCS_E_UNSUPPORTED;
     if (rows == 0) return ALCS_OK;
     if (!Y_dev || check_stored(codes_dev, scales_dev) != ALCS_OK) return ALCS_E_INVALID_ARG;
-    const int eights = (cols + 127) / 128 * 16;
-    if (rows > ((1LL << 32) - 512) / eights) return ALCS_E_UNSUPPORTED;  // a launch has less than 2^32 threads
-    const dim3 grid((unsigned)((rows * eights + 255) / 256));
-    const uint32_t *c = (const uint32_t *)codes_dev;
+    const int pieces = (cols + 127) / 128 * (dtype == ALCS_F32 ? 32 : 16);
+    if (rows > ((1LL << 32) - 512) / pieces) return ALCS_E_UNSUPPORTED;  // a launch has less than 2^32 threads
+    const dim3 grid((unsigned)((rows * pieces + 255) / 256));
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == ALCS_F32)
-        hipLaunchKernelGGL(k_mx4_dequantize<float>, grid, dim3(256), 0, st, c, scales_dev, rows, cols, eights, (float *)Y_dev);
+        hipLaunchKernelGGL(k_mx4_dequantize<float>, grid, dim3(256), 0, st, codes_dev, scales_dev, rows, cols, pieces, (float *)Y_dev);
     else if (dtype == ALCS_BF16)
-        hipLaunchKernelGGL(k_mx4_dequantize<__bf16>, grid, dim3(256), 0, st, c, scales_dev, rows, cols, eights, (__bf16 *)Y_dev);
+        hipLaunchKernelGGL(k_mx4_dequantize<__bf16>, grid, dim3(256), 0, st, codes_dev, scales_dev, rows, cols, pieces, (__bf16 *)Y_dev);
     else
-        hipLaunchKernelGGL(k_mx4_dequantize<_Float16>, grid, dim3(256), 0, st, c, scales_dev, rows, cols, eights, (_Float16 *)Y_dev);
+        hipLaunchKernelGGL(k_mx4_dequantize<_Float16>, grid, dim3(256), 0, st, codes_dev, scales_dev, rows, cols, pieces, (_Float16 *)Y_dev);
     return launched();
 }
 
