@@ -16,15 +16,15 @@ struct GradArgs {
     void *dG, *dU;
     float *sums;         // [part][2][F] or null
     int T, F, pitch;     // pitch of dG and dU, elements
-    int rows, gate, vec; // rows of a part; vec: G, U, dH may be read four elements at a time
+    int rows, gate;      // rows of a part
 };
 
-template <class T> __device__ inline void load4(const T *p, int n, int vec, float v[4]) {
-    if (vec && n >= 4) {
-        struct alignas(sizeof(T) * 4) Four { T e[4]; };
-        const Four f = *(const Four *)p;
+template <class T> __device__ inline void load4(const T *p, int n, float v[4]) {
+    if (n >= 4) {  // of any alignment
+        T e[4];
+        __builtin_memcpy(e, p, sizeof(e));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = to_float(f.e[i]);
+        for (int i = 0; i < 4; ++i) v[i] = to_float(e[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = i < n ? to_float(p[i]) : 0.0f;
@@ -44,9 +44,9 @@ template <class T, int AHEAD> __global__ __launch_bounds__(256) void k_gate_grad
         for (int r = r0 + y; r < r1; r += 4) {
             const long long at = (long long)r * a.F + c;
             float g[4], u[4], h[4], dg[4], du[4];
-            load4((const T *)a.G + at, n, a.vec, g);
-            load4((const T *)a.U + at, n, a.vec, u);
-            load4((const T *)a.dH + at, n, a.vec, h);
+            load4((const T *)a.G + at, n, g);
+            load4((const T *)a.U + at, n, u);
+            load4((const T *)a.dH + at, n, h);
             float v[4], d[4];
             gate_slopes<sizeof(T) == 4>(a.gate, g, v, d);
 #pragma unroll
@@ -56,8 +56,8 @@ template <class T, int AHEAD> __global__ __launch_bounds__(256) void k_gate_grad
                 sg[i] += dg[i];
                 su[i] += du[i];
             }
-            store4((T *)a.dG + (long long)r * a.pitch + c, dg, 4, 1);
-            store4((T *)a.dU + (long long)r * a.pitch + c, du, 4, 1);
+            store_some<4>((T *)a.dG + (long long)r * a.pitch + c, dg, 4);
+            store_some<4>((T *)a.dU + (long long)r * a.pitch + c, du, 4);
         }
     }
     if (!a.sums) return;
@@ -252,8 +252,6 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
     g.dG = workspace + s.dG; g.dU = workspace + s.dU;
     g.sums = b.dbg || b.dbu ? (float *)(workspace + s.sums) : nullptr;
     g.T = b.T; g.F = b.F; g.pitch = s.pitch; g.rows = s.rows; g.gate = b.gate;
-    const uintptr_t where = (uintptr_t)b.G | (uintptr_t)b.U | (uintptr_t)b.dH;
-    g.vec = b.F % 4 == 0 && where % (4 * sizeof(T)) == 0;
     // (many parts have wavefronts enough: 8192 x 8192, bfloat16, 123 us with one row ahead, 154 with four)
     auto grad = s.rows == 16 ? k_gate_grad<T, 4> : k_gate_grad<T, 1>;
     hipLaunchKernelGGL(grad, dim3((unsigned)((s.pitch + 255) / 256), (unsigned)s.parts), dim3(256), 0, stream, g);
@@ -276,7 +274,6 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         a.segs = 2; a.results = 1;
         a.out[0] = b.dX;
         a.ldo = b.D;
-        a.vec = rows_of_eights({b.dX}, b.D);
         const Plan p = plan_tiles(dx_shape(E, b.T, b.D, s.pitch), INT64_MAX, cus);
         if ((rc = launch_tiles<E, T, false, true, false>(a, p, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
@@ -291,7 +288,6 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         a.segs = 1; a.results = 2;
         a.out[0] = b.dWg; a.out[1] = b.dWu;
         a.ldo = b.D;
-        a.vec = rows_of_eights({b.dWg, b.dWu}, b.D);
         const Plan p = plan_tiles(dw_shape(E, b.T, b.D, b.F), INT64_MAX, cus);
         if ((rc = launch_tiles<E, T, true, true, false>(a, p, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
     }
@@ -347,7 +343,6 @@ extern "C" int alcs_gated_ff(const void *X_dev, long long ldx, const void *Wg_de
     a.out[0] = H_dev; a.pre[0] = G_dev; a.pre[1] = U_dev;
     a.ldo = F;
     a.act = gate;
-    a.vec = rows_of_eights({H_dev, G_dev, U_dev}, F);
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == ALCS_F32) return gated_as<kF32>(a, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
     if (dtype == ALCS_BF16) return gated_as<kBF16>(a, (char *)workspace_dev, workspace_bytes, cus, xcds, st);

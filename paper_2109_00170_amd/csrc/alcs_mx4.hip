@@ -178,7 +178,6 @@ extern "C" int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scal
     a.out[0] = Y_dev;
     a.ldo = N;
     a.act = activation;
-    a.vec = rows_of_eights({Y_dev}, N);
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == ALCS_F32) return linear_as<float>(a, workspace_dev, workspace_bytes, cus, xcds, st);
     if (dtype == ALCS_BF16) return linear_as<__bf16>(a, workspace_dev, workspace_bytes, cus, xcds, st);

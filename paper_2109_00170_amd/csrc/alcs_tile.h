@@ -143,15 +143,16 @@ struct Args {
     int segs, results;
     int tiles_m, tiles_n, splits, ktiles;  // ktiles: K tiles of a segment
     unsigned total, per_xcd, xcds;
-    float *partial;      // splits > 1: [split][plane][M][N] sums
+    float *partial;      // splits > 1: [split][plane][M][sum_pitch(N)] sums
     const float *bias[2];
     void *out[2];        // the result(s); gated: H
     void *pre[2];        // gated: G and U where the caller keeps them, or null
     long long ldo;       // elements from one row of out (and pre) to the next
     int act;             // alcs_activation, or alcs_gate for a gated product
-    int vec;             // out and pre may be written eight elements at a time
 };
 
+// Rows of sums start at 16-byte addresses.
+__host__ __device__ constexpr int sum_pitch(int n) { return (n + 3) & ~3; }
 __device__ const v4i g_zeros[4] = {};  // what pieces beyond K read
 
 // Direct load of 16 (or 4) bytes a lane from global memory into LDS at lds + lane * 16 (4).  Written out,
@@ -303,23 +304,28 @@ template <int N, class F> __device__ inline void each(F &&f) { each_of(std::make
 
 // ------------------------------------------------------------------------------ what follows the sum
 
-template <class T> __device__ inline void store4(T *p, const float v[4], int n, int vec) {
-    if (vec && n >= 4) {
-        struct alignas(sizeof(T) * 4) Four { T e[4]; } f;
+// N neighbours, of which `left` are inside the row, in one store (or two of 16 bytes) where all are: of any alignment, which
+// the memory system takes.
+template <int N, class T> __device__ inline void store_some(T *p, const float *v, int left) {
+    T e[N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f.e[i] = (T)v[i];
-        *(Four *)p = f;
+    for (int i = 0; i < N; ++i) e[i] = (T)v[i];
+    if (left >= N) {
+        __builtin_memcpy(p, e, sizeof(e));
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = (T)v[i];
+        for (int i = 0; i < N; ++i)
+            if (i < left) p[i] = e[i];
     }
 }
-template <class T> __device__ inline void store8(T *p, const float (&v)[8]) {
-    struct alignas(16) Eight { T e[8]; } f;
+template <int N> __device__ inline void load_some(const float *p, float *v, int left) {
+    if (left >= N) {
+        __builtin_memcpy(v, p, N * sizeof(float));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f.e[i] = (T)v[i];
-    *(Eight *)p = f;
+        for (int i = 0; i < N; ++i)
+            if (i < left) v[i] = p[i];
+    }
 }
 // four neighbours of a row: bias, activation, rounding (once, to the result's type)
 template <class T> __device__ inline void finish_plain(const Args &a, int result, long long m, int n, v4f c) {
@@ -328,7 +334,7 @@ template <class T> __device__ inline void finish_plain(const Args &a, int result
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = activate(a.act, c[i] + (a.bias[0] && i < left ? a.bias[0][n + i] : 0.0f));
-    store4((T *)a.out[result] + m * a.ldo + n, v, left, a.vec);
+    store_some<4>((T *)a.out[result] + m * a.ldo + n, v, left);
 }
 template <class T> __device__ inline void finish_gated(const Args &a, long long m, int n, v4f g, v4f u) {
     const int left = a.N - n;
@@ -341,10 +347,10 @@ template <class T> __device__ inline void finish_gated(const Args &a, long long 
         h[i] = gate_value<sizeof(T) == 4>(a.act, gg[i]) * uu[i];
     }
     const long long at = m * a.ldo + n;
-    store4((T *)a.out[0] + at, h, left, a.vec);
+    store_some<4>((T *)a.out[0] + at, h, left);
     if (a.pre[0]) {
-        store4((T *)a.pre[0] + at, gg, left, a.vec);
-        store4((T *)a.pre[1] + at, uu, left, a.vec);
+        store_some<4>((T *)a.pre[0] + at, gg, left);
+        store_some<4>((T *)a.pre[1] + at, uu, left);
     }
 }
 
@@ -359,8 +365,7 @@ template <class T, bool GATED, int COLS>
 __device__ inline void finish_rows(const Args &a, char *slab, int rows, int m0, int n0, int result, int split, int lane) {
     constexpr bool kExact = sizeof(T) == 4;
     constexpr int kOut = GATED ? COLS / 2 : COLS, kPitch = COLS * 4;
-    if (a.partial) {
-        // four neighbours a lane where rows of the sums start at 16-byte addresses
+    if (a.partial) {  // four neighbours a lane
         constexpr int kLanes = COLS / 4;
         const int piece = lane % kLanes, plane = GATED && piece >= kLanes / 2;
         const int n = n0 + piece % (kOut / 4) * 4, left = a.N - n;
@@ -369,74 +374,51 @@ __device__ inline void finish_rows(const Args &a, char *slab, int rows, int m0, 
         for (int it = 0; it < rows * kLanes / 64; ++it) {
             const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
             const v4f v = *(const v4f *)slab_at(slab, kPitch, row, piece);
-            if (m >= a.M || left <= 0) continue;
-            float *p = a.partial + (plane0 * a.M + m) * a.N + n;
-            if (a.N % 4 == 0) *(v4f *)p = v;
-            else
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e < left) p[e] = v[e];
+            if (m < a.M && left > 0) *(v4f *)(a.partial + (plane0 * a.M + m) * sum_pitch(a.N) + n) = v;
         }
         return;
     }
-    if (a.vec) {
-        constexpr int kLanes = kOut / 8;
-        const int n = n0 + lane % kLanes * 8, left = a.N - n;
-        float b0[8], b1[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            b0[e] = a.bias[0] && left > 0 ? a.bias[0][n + e] : 0.0f;
-            b1[e] = GATED && a.bias[1] && left > 0 ? a.bias[1][n + e] : 0.0f;
-        }
+    constexpr int kLanes = kOut / 8;  // eight neighbours (of both projections) a lane
+    const int n = n0 + lane % kLanes * 8, left = a.N - n;
+    const bool inside = m0 + rows <= a.M && n0 + kOut <= a.N;  // all of the wavefront's
+    float b0[8] = {}, b1[8] = {};
+    if (a.bias[0]) load_some<8>(a.bias[0] + n, b0, left);
+    if (GATED && a.bias[1]) load_some<8>(a.bias[1] + n, b1, left);
 #pragma clang loop unroll_count(2)
-        for (int it = 0; it < rows * kLanes / 64; ++it) {
-            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
-            float c[8], u[8], h[8];
+    for (int it = 0; it < rows * kLanes / 64; ++it) {
+        const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
+        float c[8], u[8], h[8];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int piece = lane % kLanes * 2 + k;
-                const v4f v = *(const v4f *)slab_at(slab, kPitch, row, piece);
-                const v4f w = GATED ? *(const v4f *)slab_at(slab, kPitch, row, piece + COLS / 8) : v;
+        for (int k = 0; k < 2; ++k) {
+            const int piece = lane % kLanes * 2 + k;
+            const v4f v = *(const v4f *)slab_at(slab, kPitch, row, piece);
+            const v4f w = GATED ? *(const v4f *)slab_at(slab, kPitch, row, piece + COLS / 8) : v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    c[4 * k + e] = v[e] + b0[4 * k + e];
-                    u[4 * k + e] = w[e] + b1[4 * k + e];
-                }
-            }
-            const long long at = m * a.ldo + n;
-            if (GATED) {
-                gate_values<kExact>(a.act, c, h);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] *= u[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = activate(a.act, c[e]);
-            }
-            if (m >= a.M || left <= 0) continue;
-            store8((T *)a.out[GATED ? 0 : result] + at, h);
-            if (GATED && a.pre[0]) {
-                store8((T *)a.pre[0] + at, c);
-                store8((T *)a.pre[1] + at, u);
+            for (int e = 0; e < 4; ++e) {
+                c[4 * k + e] = v[e] + b0[4 * k + e];
+                u[4 * k + e] = w[e] + b1[4 * k + e];
             }
         }
-        return;
-    }
-    constexpr int kLanes = kOut < 64 ? kOut : 64;
-    for (int first = 0; first < kOut; first += kLanes) {
-        const int c = first + lane % kLanes, n = n0 + c;
-        const bool in = n < a.N;
-        const float b0 = a.bias[0] && in ? a.bias[0][n] : 0.0f, b1 = GATED && a.bias[1] && in ? a.bias[1][n] : 0.0f;
-#pragma clang loop unroll_count(4)
-        for (int it = 0; it < rows * kLanes / 64; ++it) {
-            const int row = it * (64 / kLanes) + lane / kLanes, m = m0 + row;
-            const float g = *(const float *)(slab_at(slab, kPitch, row, c / 4) + c % 4 * 4) + b0;
-            const float u = GATED ? *(const float *)(slab_at(slab, kPitch, row, (c + kOut) / 4) + c % 4 * 4) + b1 : 0.0f;
-            const long long at = m * a.ldo + n;
-            if (m >= a.M || !in) continue;
-            ((T *)a.out[GATED ? 0 : result])[at] = (T)(GATED ? gate_value<kExact>(a.act, g) * u : activate(a.act, g));
+        const long long at = m * a.ldo + n;
+        if (GATED) {
+            gate_values<kExact>(a.act, c, h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] *= u[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = activate(a.act, c[e]);
+        }
+        if (inside) {
+            store_some<8>((T *)a.out[GATED ? 0 : result] + at, h, 8);
             if (GATED && a.pre[0]) {
-                ((T *)a.pre[0])[at] = (T)g;
-                ((T *)a.pre[1])[at] = (T)u;
+                store_some<8>((T *)a.pre[0] + at, c, 8);
+                store_some<8>((T *)a.pre[1] + at, u, 8);
+            }
+        } else if (m < a.M && left > 0) {
+            store_some<8>((T *)a.out[GATED ? 0 : result] + at, h, left);
+            if (GATED && a.pre[0]) {
+                store_some<8>((T *)a.pre[0] + at, c, left);
+                store_some<8>((T *)a.pre[1] + at, u, left);
             }
         }
     }
@@ -887,22 +869,18 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
 // The sums of a split K, added in the order of the splits; a thread has four neighbours of a row.
 template <class T, bool GATED> __global__ __launch_bounds__(256) void k_join(const Args a) {
     const int quads = (a.N + 3) / 4;
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    const unsigned at = blockIdx.x * 256 + threadIdx.x;
     const int planes = GATED ? 1 : a.results;
     if (at >= (long long)planes * a.M * quads) return;
-    const int n = (int)(at % quads) * 4;
-    const long long row = at / quads;  // plane * M + m
-    const long long plane = (long long)(GATED ? 2 : a.results) * a.M * a.N;
-    const int left = min(4, a.N - n);
+    const int n = (int)(at % (unsigned)quads) * 4;
+    const long long row = at / (unsigned)quads;  // plane * M + m
+    const int pitch = sum_pitch(a.N);
+    const long long plane = (long long)(GATED ? 2 : a.results) * a.M * pitch;
     v4f s[2] = {};
+#pragma clang loop unroll_count(4)
     for (int k = 0; k < a.splits; ++k)
 #pragma unroll
-        for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-            const float *p = a.partial + k * plane + (row + (long long)h * a.M) * a.N + n;
-            if (a.N % 4 == 0) s[h] += *(const v4f *)p;
-            else
-                for (int i = 0; i < left; ++i) s[h][i] += p[i];
-        }
+        for (int h = 0; h < (GATED ? 2 : 1); ++h) s[h] += *(const v4f *)(a.partial + k * plane + (row + (long long)h * a.M) * pitch + n);
     if (GATED) finish_gated<T>(a, row, n, s[0], s[1]);
     else finish_plain<T>(a, (int)(row / a.M), row % a.M, n, s[0]);
 }
@@ -1008,12 +986,6 @@ __global__ __launch_bounds__(512, 2) void k_few(const Args a) {
 
 // ------------------------------------------------------------------------------ launches
 
-// whether rows of `columns` packed elements may be written eight at a time (null pointers aside)
-inline int rows_of_eights(std::initializer_list<const void *> outs, int columns) {
-    uintptr_t all = 0;
-    for (const void *p : outs) all |= (uintptr_t)p;
-    return columns % 8 == 0 && all % 16 == 0;
-}
 // Kinds of tiles: 256 x 256 (k_big), 128 x 128 and 64 x 128 (k_mid).
 enum Kind { kBig = 0, k128 = 1, k64 = 2 };
 struct Plan {
@@ -1035,13 +1007,14 @@ inline Plan plan_of(const Shape &s, int kind, int splits) {
     p.tiles_m = (int)up(s.M, rows);
     p.tiles_n = (int)up(s.N, s.gated ? cols / 2 : cols);
     p.splits = splits;
-    p.workspace = splits > 1 ? (long long)splits * (s.gated ? 2 : s.results) * s.M * s.N * 4 : 0;
+    p.workspace = splits > 1 ? (long long)splits * (s.gated ? 2 : s.results) * s.M * sum_pitch((int)s.N) * 4 : 0;
     return p;
 }
 // What a plan takes, in microseconds, as measured on MI355X: a launch with its first loads and its stores, then so much
 // for a K tile of 128 bytes a row, of one workgroup alone on its compute unit and of two.  Small tiles of 16 bits
 // alone: 0.32 and 0.50; where the sum runs over rows (transposing reads) a third more; 256 x 256 tiles run at the
-// card's power limit.  A split costs another launch and the sums' way to memory and back at 4 TB/s.
+// card's power limit.  A split costs another launch and the sums' way out and back at 8 TB/s (they
+// stay in the last cache).
 //   333 x 1000 -> 2 x 2728 (bfloat16): 128 x 128 tiles 13.7 us, 64 rows 15.0 (258 tiles), 128 x 128 in three parts 22
 //   500 x 512 -> 2 x 1365 (float32): 64 rows 23.7 us, 128 x 128 40.2
 //   512 x 8192 -> 1024 (bfloat16): 64 rows in eight parts 30 us, in one 62, 128 x 128 in eight parts 31, 256 x 256 178
@@ -1052,7 +1025,8 @@ inline double time_of(const Shape &s, const Plan &p, int cus) {
     static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}};
     static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}};
     const Cost &c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[p.kind];
-    const double strided = s.strided && s.E != kF32 && p.kind != kBig ? 1.3 : 1.0;
+    const bool strided = s.strided && s.E != kF32 && p.kind != kBig;
+    const double alone = c.alone * (strided ? 1.3 : 1.0), two = c.two * (strided && p.kind == k64 ? 1.07 : 1.0);
     const long long tiles = (long long)p.tiles_m * p.tiles_n * s.results * p.splits;
     const double depth = (double)(long long)(p.ktiles * s.segs / p.splits);
     double t;
@@ -1060,10 +1034,10 @@ inline double time_of(const Shape &s, const Plan &p, int cus) {
         t = c.fixed + (double)up(tiles, cus) * (depth * c.alone + 6);
     } else {
         const long long full = tiles / (2 * cus), left = tiles % (2 * cus);
-        t = c.fixed + (double)full * (depth * c.two * strided + 2);
-        if (left) t += left <= cus ? depth * c.alone * strided : depth * c.two * std::max(1.0, strided * 0.85);
+        t = c.fixed + (double)full * (depth * two + 2);
+        if (left) t += depth * (left <= cus ? alone : two);
     }
-    return p.splits > 1 ? t + 4 + (double)p.workspace * 2 / 4e6 : t;
+    return p.splits > 1 ? t + 4 + (double)p.workspace * 2 / 8e6 : t;
 }
 // workspace: bytes there are for a split.
 inline Plan plan_tiles(const Shape &s, long long workspace, int cus) {
@@ -1073,7 +1047,8 @@ inline Plan plan_tiles(const Shape &s, long long workspace, int cus) {
         if (kind == kBig && s.E == kF32) continue;
         for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
             const Plan p = plan_of(s, kind, splits);
-            if (splits > 1 && (kind == kBig || p.workspace > workspace || p.ktiles * s.segs < 2 * splits)) break;
+            // (a launch that joins has less than 2^32 threads, of four sums each)
+            if (splits > 1 && (kind == kBig || p.workspace > workspace || p.ktiles * s.segs < 2 * splits || s.results * s.M * s.N >= 1LL << 33)) break;
             const double t = time_of(s, p, cus);
             if (best.tiles_m == 0 || t < least) { best = p; least = t; }
         }
