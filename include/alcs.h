@@ -579,10 +579,13 @@ typedef enum alcs_gate {
  *   overwritten.  G_dev and U_dev [T, F], or both NULL, receive G and U (rounded to `dtype`; H is made from
  *   the unrounded ones) for the gradients.  gate: an alcs_gate value (ALCS_E_INVALID_ARG otherwise).
  *   workspace_dev: as for alcs_mx4_linear, alcs_gated_ff_workspace_bytes(T, D, F, dtype) bytes, or NULL.  It also takes
- *   copies of operands whose rows do not start at 16-byte addresses (or end there, or lie more than 4 MB apart); without
- *   room for them such a call of many rows is several times slower.
- *   T = 0 is a no-op; sizes at most 2^26 (ALCS_E_UNSUPPORTED beyond).  Asynchronous on `stream`, nothing allocated; equal calls give equal
- *   bits, a row's result may differ in its last bits with the number of rows it is computed with.
+ *   copies of operands whose rows do not start at 16-byte addresses, or end there, or lie more than 4 MB apart; without
+ *   room for them such a call of many rows is several times slower, and has fewer than 2^32 results.  (The size that is
+ *   asked for holds them where D makes rows end elsewhere.  Views of other tensors that start elsewhere or lie far apart
+ *   need (T + 2 F) (D + 8) elements and 1024 bytes more to be copied.)
+ *   T = 0 is a no-op; T at most 2^26, D and F at most 2^20, fewer than 2^24 tiles of 64 x 64 (ALCS_E_UNSUPPORTED
+ *   beyond).  Asynchronous on `stream`, nothing allocated; equal calls give equal bits, a row's result may differ in
+ *   its last bits with the number of rows it is computed with.
  *
  * alcs_gated_ff_backward: from dH_dev [T, F], the gradient of a number with respect to H, and the forward's
  * operands and G, U:

@@ -52,7 +52,7 @@ template <class T, int AHEAD> __global__ __launch_bounds__(256) void k_gate_grad
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 du[i] = i < n ? h[i] * v[i] : 0.0f;
-                dg[i] = i < n ? h[i] * u[i] * d[i] : 0.0f;
+                dg[i] = i < n ? h[i] * (u[i] * d[i]) : 0.0f;  // (u * d first: with a slope of 0 no product overflows)
                 sg[i] += dg[i];
                 su[i] += du[i];
             }
@@ -106,7 +106,9 @@ template <class T> int fill_zero(void *p, long long n, hipStream_t stream) {
 
 // ------------------------------------------------------------------------------ host side
 
-constexpr int kMaxSize = 1 << 26;  // rows, columns: numbers of pieces and threads stay inside 32 bits
+constexpr int kMaxRows = 1 << 26;  // numbers of rows and threads stay inside 32 bits
+constexpr int kMaxWidth = 1 << 20;  // D and F: rows of copies, of dG and of dU are near ones, in float32 too
+static_assert(kMaxWidth * 4LL <= kNearPitch, "a tile's offsets are 32 bits");
 
 // Rows that the tiles' direct loads take: they start at 16-byte addresses, hold whole 16-byte pieces and lie at most
 // kNearPitch apart.
@@ -297,7 +299,7 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
 int check(int T, int D, int F, int dtype, int gate) {
     if (T < 0 || D <= 0 || F <= 0) return ALCS_E_INVALID_ARG;
     if (dtype < ALCS_F32 || dtype > ALCS_F16 || gate < ALCS_GATE_NONE || gate > ALCS_GATE_SIGMOID) return ALCS_E_INVALID_ARG;
-    return T > kMaxSize || D > kMaxSize || F > kMaxSize ? ALCS_E_UNSUPPORTED : ALCS_OK;
+    return T > kMaxRows || D > kMaxWidth || F > kMaxWidth ? ALCS_E_UNSUPPORTED : ALCS_OK;
 }
 
 }  // namespace tile

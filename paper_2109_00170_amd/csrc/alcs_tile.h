@@ -9,12 +9,16 @@
 //
 // Operands are brought into LDS by the load that writes there directly (16 bytes a lane, a wavefront's 1024
 // bytes in lane order), so the arrangement against bank conflicts is made on the global side: which piece a
-// lane fetches.  Two K tiles are in LDS: while one is multiplied, the other is on its way.
+// lane fetches.  Two or three K tiles are in LDS: while one is multiplied, the others are on their way.
 //
 // Layouts.  "K contiguous" (rows of A and B as a linear layer has them): [row][128 bytes], the 16-byte
 // piece c of row r at position c ^ (r & 7).  "K strided" (the operands of a gradient, whose sum runs over
 // rows): [k][row], read transposed - by the LDS load that transposes 16-bit values, float by float for
 // float32 -, in units of 16 rows whose positions are exchanged among the k that one load reads together.
+//
+// Three kernels: k_big (256 x 256 tiles) for large products, k_mid (64 or 128 x 128) for those of the middle, with K
+// shared out and k_join to add the parts where there are few tiles, k_few for a token or a few; plan_tiles() and
+// few_rows() choose, by what was measured.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -99,8 +103,9 @@ template <bool EXACT> __device__ inline void gate_both(int gate, float g, float 
         }
         case ALCS_GATE_GELU_TANH: {
             const float s = sigmoid<EXACT>(2.0f * kGeluA * (g + kGeluB * g * g * g));
+            const float b = fminf(g * g, 1e6f);  // beyond it s (1 - s) is 0, and g * g may be infinite
             v = g * s;
-            d = s + g * s * (1.0f - s) * 2.0f * kGeluA * (1.0f + 3.0f * kGeluB * g * g);
+            d = s + g * (s * (1.0f - s)) * 2.0f * kGeluA * (1.0f + 3.0f * kGeluB * b);
             break;
         }
         case ALCS_GATE_SIGMOID: { const float s = sigmoid<EXACT>(g); v = s; d = s * (1.0f - s); break; }
@@ -293,8 +298,8 @@ __device__ inline void claim_accumulators() {
                  ALCS_TEN(22), ALCS_TEN(23), ALCS_TEN(24), "a250", "a251", "a252", "a253", "a254", "a255");
 }
 #undef ALCS_TEN
-// A register that a vector instruction wrote may be a matrix instruction's operand two states later, a matrix
-// instruction's result may be read 19 states later at the latest.
+// A register that a vector instruction wrote may be a matrix instruction's operand two states later; a matrix
+// instruction's result may be read after 19 states, whichever instruction it was.
 __device__ inline void operands_ready() { asm volatile("s_nop 1"); }
 __device__ inline void matrix_done() { asm volatile("s_nop 15\n\ts_nop 15"); }
 
@@ -888,9 +893,11 @@ template <class T, bool GATED> __global__ __launch_bounds__(256) void k_join(con
 // ------------------------------------------------------------------------------ few rows
 
 // 16 * MF rows of A (a token, a few requests) a workgroup: the weights are read once and the product is bound by
-// their bytes, so nothing is staged.  Operands of any alignment and distance.  A workgroup has 16 columns (of both projections where GATED); its wavefronts
-// share out K in pieces of 256 bytes a row, read their fragments straight from memory, four steps ahead of
-// the multiply, and add their sums through LDS in a fixed order.  Rows of A beyond M read the last row.
+// their bytes, so nothing is staged.  Operands of any alignment and distance, and so also the way of many rows whose
+// operands the tiles do not take, where there is no room for copies.  A workgroup has 16 columns (of both projections
+// where GATED); its wavefronts share out K in pieces of 256 bytes a row, read their fragments straight from memory,
+// four steps ahead of the multiply, and add their sums through LDS in a fixed order.  Rows of A beyond M read the last
+// row.
 template <int E, bool ALIGNED> __device__ inline v4i piece_of(const char *row, int k, int K) {
     constexpr int kElems = per16(E);
     v4i v = {0, 0, 0, 0};

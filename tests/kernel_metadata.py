@@ -14,25 +14,6 @@ LLVM = "/opt/rocm/llvm/bin"
 MAGIC = b"__CLANG_OFFLOAD_BUNDLE__"
 
 
-def code_objects():
-    """The gfx950 code objects of libalcs.so, as bytes."""
-    with tempfile.TemporaryDirectory() as d:
-        section = os.path.join(d, "fatbin")
-        subprocess.check_call(["objcopy", "-O", "binary", "--only-section=.hip_fatbin", alcs.library_path(), section])
-        with open(section, "rb") as f:
-            data = f.read()
-    at = data.find(MAGIC)
-    while at >= 0:
-        entry = at + 32
-        for _ in range(struct.unpack_from("<Q", data, at + 24)[0]):
-            offset, size, length = struct.unpack_from("<QQQ", data, entry)
-            target = data[entry + 24:entry + 24 + length].decode()
-            entry += 24 + length
-            if "gfx950" in target and size:
-                yield data[at + offset:at + offset + size]
-        at = data.find(MAGIC, at + len(MAGIC))
-
-
 @functools.lru_cache(None)
 def kernels():
     """{demangled name without arguments: Kernel}"""

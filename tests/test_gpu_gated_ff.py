@@ -163,6 +163,65 @@ def test_backward_parts_of_the_gradients():
     assert same(again[0], outs[0])
 
 
+@pytest.mark.parametrize("kind", GATES)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_slopes_far_out(kind, dtype):
+    # one row and one column, so that dWg is dG and dWu is dU: far from 0 every gate is flat or the line g
+    top = 6e4 if dtype == torch.float16 else 3e38
+    far = torch.tensor([200.0, 1e4, top], dtype=dtype)
+    G = torch.cat([far, -far]).view(1, 6).cuda()
+    one = torch.ones(6, 1, dtype=dtype, device="cuda")
+    big = 2.0 ** 10 if dtype == torch.float16 else 2.0 ** 100
+    for u, h in ((0.5, 2.0), (big, 1 / big), (1 / big, 1.0)):
+        U, dH = torch.full_like(G, u), torch.full_like(G, h)
+        dWg, dWu = torch.empty_like(one), torch.empty_like(one)
+        alcs.alcs_gated_ff_backward(one[:1], one, one, G, U, dH, None, dWg, dWu, None, None, gate=kind,
+                                    workspace=scratch(alcs.alcs_gated_ff_backward_workspace_bytes(1, 1, 6, dtype)))
+        up, down = {"none": (1, 1), "sigmoid": (0, 0)}.get(kind, (1, 0))
+        assert dWg.view(-1).tolist() == [u * h * up] * 3 + [u * h * down] * 3, (kind, u, h)
+    # and where both factors' product would overflow, but the slope is 0
+    if kind not in ("none", "sigmoid") and dtype != torch.float16:
+        alcs.alcs_gated_ff_backward(one[:1], one, one, G, torch.full_like(G, big), torch.full_like(G, big), None, dWg, dWu, None, None,
+                                    gate=kind, workspace=scratch(alcs.alcs_gated_ff_backward_workspace_bytes(1, 1, 6, dtype)))
+        assert dWg.view(-1)[3:].tolist() == [0.0] * 3
+
+
+def apart(t, pitch, offset):
+    """t's values as rows `pitch` elements apart that start `offset` elements into a tensor."""
+    whole = torch.zeros(offset + (t.shape[0] - 1) * pitch + t.shape[1], dtype=t.dtype, device="cuda")
+    v = torch.as_strided(whole, t.shape, (pitch, 1), offset)
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("pitch,offset", [(72, 0), (72, 1), (65, 0), (2 ** 21 + 8, 0), (2 ** 21 + 9, 3)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_that_have_to_be_copied(dtype, pitch, offset):
+    # rows of whole pieces that start elsewhere or lie far apart: with room for copies, without, and without a workspace
+    T, D, F = 150, 64, 100
+    X, Wg, Wu, bg, bu = operands(T, D, F, dtype, 55)
+    n = alcs.alcs_gated_ff_workspace_bytes(T, D, F, dtype)
+    x, a, b = (apart(t, pitch, offset) for t in (X, Wg, Wu))
+    for xs, ws in (((x, Wg, Wu), n), ((X, a, Wu), n), ((x, a, b), n), ((x, a, b), n + 8 * (T + 2 * F) * (D + 8)), ((X, Wg, b), 0)):
+        run_forward(*xs, bg, bu, "silu", True, scratch(ws) if ws else None, "%d %d" % (pitch, offset))
+    G, U, dH = (normal(T, F, seed=i, dtype=dtype) for i in (5, 6, 7))
+    ws = scratch(alcs.alcs_gated_ff_backward_workspace_bytes(T, D, F, dtype))
+    want, got = ([torch.empty(*s, dtype=dtype, device="cuda") for s in ((T, D), (F, D), (F, D), (F,), (F,))] for _ in range(2))
+    alcs.alcs_gated_ff_backward(X, Wg, Wu, G, U, dH, *want, workspace=ws)
+    for ops in ((x, Wg, b), (x, a, b)):
+        alcs.alcs_gated_ff_backward(*ops, G, U, dH, *got, workspace=ws)
+        assert all(same(p, q) for p, q in zip(want, got))
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2])
+@pytest.mark.parametrize("T,D,F", [(70, 2 ** 20, 3), (70, 2 ** 20 - 1, 3), (70, 3, 2 ** 20), (70, 8, 2 ** 20 - 3)])
+def test_widest(T, D, F, dtype):
+    X, Wg, Wu, bg, bu = operands(T, D, F, dtype, 9)
+    run_forward(X, Wg, Wu, bg, bu, "silu", False, scratch(alcs.alcs_gated_ff_workspace_bytes(T, D, F, dtype)), "widest")
+    del X, Wg, Wu
+    run_backward(T, D, F, dtype, "silu", 19, "widest")
+
+
 def test_no_rows():
     X, Wg, Wu, bg, bu = operands(4, 32, 16, torch.bfloat16, 1)
     empty = torch.empty(0, 16, dtype=torch.bfloat16, device="cuda")
@@ -180,6 +239,40 @@ def test_a_row_that_is_not_finite_stays_alone():
         alcs.alcs_gated_ff(X, Wg, Wu, bg, bu, H)
         bad = torch.isnan(H)
         assert bool(bad[3].all()) and int(bad.sum()) == 24
+
+
+def test_a_gradient_that_is_not_finite_stays_alone():
+    # a NaN in one row of dH: that row of dX, that column's gradients, and nothing beside them
+    T, D, F = 100, 40, 24
+    X, Wg, Wu, _, _ = operands(T, D, F, torch.bfloat16, 1)
+    G, U, dH = (normal(T, F, seed=i, dtype=torch.bfloat16) for i in (5, 6, 7))
+    dH[3, 5] = float("nan")
+    outs = [torch.empty(*s, dtype=torch.bfloat16, device="cuda") for s in ((T, D), (F, D), (F, D), (F,), (F,))]
+    alcs.alcs_gated_ff_backward(X, Wg, Wu, G, U, dH, *outs, workspace=scratch(alcs.alcs_gated_ff_backward_workspace_bytes(T, D, F, torch.bfloat16)))
+    for o, row, n in zip(outs, (3, 5, 5, 5, 5), (D, D, D, 1, 1)):
+        bad = torch.isnan(o)
+        assert bool(bad[row].all()) and int(bad.sum()) == n
+
+
+def test_two_calls_at_once():
+    # on two streams, each with a workspace of its own
+    T, D, F = 700, 1000, 520
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    sets = [operands(T, D, F, torch.bfloat16, seed) for seed in (1, 21)]
+    wants = [run_forward(*o, "silu", True, None, "alone") for o in sets]
+    n = alcs.alcs_gated_ff_workspace_bytes(T, D, F, torch.bfloat16)
+    spaces, outs = [scratch(n) for _ in sets], [torch.empty_like(w) for w in wants]
+    singles = []
+    for o, ws in zip(sets, spaces):
+        h = torch.empty_like(wants[0])
+        alcs.alcs_gated_ff(*o, h, workspace=ws)
+        singles.append(h)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for o, ws, h, st in zip(sets, spaces, outs, (s1, s2)):
+            alcs.alcs_gated_ff(*o, h, workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    assert all(same(a, b) for a, b in zip(outs, singles))
 
 
 def test_equal_calls_and_another_stream():

@@ -82,3 +82,16 @@ def test_tensors_that_are_not_on_a_gpu_are_refused():
                  lambda: alcs.alcs_gated_ff_backward(x, x, x, h, h, h, x, x, x, None, None)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_sizes_beyond_the_limits():
+    f, b = lib().alcs_gated_ff, lib().alcs_gated_ff_backward
+    for T, D, F in ((2 ** 26 + 1, 8, 8), (100, 2 ** 20 + 1, 8), (100, 8, 2 ** 20 + 8)):
+        for dtype in (0, 1, 2):
+            assert f(P, L(D), P, L(D), P, L(D), None, None, P, None, None, T, D, F, dtype, 2, None, L(0), None) == UNSUPPORTED
+            assert b(P, L(D), P, L(D), P, L(D), P, P, P, P, P, P, P, P, T, D, F, dtype, 2, P, L(2 ** 60), None) == UNSUPPORTED
+            assert lib().alcs_gated_ff_workspace_bytes(T, D, F, dtype) == UNSUPPORTED
+            assert lib().alcs_gated_ff_backward_workspace_bytes(T, D, F, dtype) == UNSUPPORTED
+    for M, N, K in ((2 ** 26 + 1, 8, 128), (8, 2 ** 26 + 1, 128), (8, 8, 2 ** 23 + 128)):
+        assert lib().alcs_mx4_linear(P, P, P, P, None, P, M, N, K, 0, 0, None, L(0), None) == UNSUPPORTED
+        assert lib().alcs_mx4_linear_workspace_bytes(M, N, K) == UNSUPPORTED

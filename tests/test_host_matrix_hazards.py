@@ -5,16 +5,36 @@ states later at the earliest; an accumulator is read no earlier than behind the 
 those instructions, the clearing and the reading of each accumulator once touches accumulation registers."""
 import os
 import re
+import struct
 import subprocess
 import tempfile
 
 import pytest
 
 import paper_2109_00170_amd as alcs
-from kernel_metadata import LLVM, code_objects
+from kernel_metadata import LLVM, MAGIC
 
 pytestmark = pytest.mark.skipif(not (os.path.exists(os.path.join(LLVM, "llvm-objdump")) and os.path.exists(alcs.library_path())),
                                 reason="needs the built library and llvm-objdump")
+
+
+def code_objects():
+    """The gfx950 code objects of libalcs.so, as bytes."""
+    with tempfile.TemporaryDirectory() as d:
+        section = os.path.join(d, "fatbin")
+        subprocess.check_call(["objcopy", "-O", "binary", "--only-section=.hip_fatbin", alcs.library_path(), section])
+        with open(section, "rb") as f:
+            data = f.read()
+    at = data.find(MAGIC)
+    while at >= 0:
+        entry = at + 32
+        for _ in range(struct.unpack_from("<Q", data, at + 24)[0]):
+            offset, size, length = struct.unpack_from("<QQQ", data, entry)
+            target = data[entry + 24:entry + 24 + length].decode()
+            entry += 24 + length
+            if "gfx950" in target and size:
+                yield data[at + offset:at + offset + size]
+        at = data.find(MAGIC, at + len(MAGIC))
 
 
 def registers(text):
