@@ -622,7 +622,10 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
 
 // BM x 128 (64 or 128 rows), NS K tiles in LDS.  A K tile is two steps; the fragments of the next step are read and the
 // pieces of a later tile sent for between the matrix instructions of this one, so that a wavefront waits for neither.
-// One barrier a tile, in front of its second step, as in k_big.  Two workgroups share a compute unit.
+// One barrier a tile, in front of its second step, as in k_big.  Two workgroups share a compute unit; 128 rows whose
+// tiles are no more than the card has units have all of its LDS, and with four K tiles there the weights of a deep product
+// arrive as fast as memory has them: 65 x 4096 -> 2 x 16384 (bfloat16) 44 us (6.2 TB/s), with two 62; 256 x 4096 ->
+// 2 x 8192 39 and 47.  (Of 16 K tiles, 512 x 1024 -> 2 x 4096, two are faster: 13.2 us, four 13.7.)
 template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 2) void k_mid(const Args a) {
     typedef Feed<E, BM, 128, AK, BK, GATED> Feeds;
     constexpr int FM = BM / 32, FN = 4, kA = Feeds::kA, kB = Feeds::kB, kSA = Feeds::kSA, kBuf = Feeds::kBuf;
@@ -1072,7 +1075,7 @@ inline int launched() {
 
 template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> int launch_mid(Args &a, hipStream_t stream) {
     constexpr int lds = NS * Feed<E, BM, 128, AK, BK, GATED>::kBuf;
-    static_assert(lds <= 80 * 1024, "two workgroups on a compute unit");
+    static_assert(lds <= (NS > 3 ? 160 : 80) * 1024, "two workgroups on a compute unit, one where NS is more than 3");
     auto kern = k_mid<E, T, BM, NS, AK, BK, GATED>;
     const int rc = allow_lds((const void *)kern, lds);
     if (rc != ALCS_OK) return rc;
@@ -1100,7 +1103,10 @@ int launch_tiles(Args a, const Plan &plan, void *workspace, int cus, int xcds, h
     a.xcds = (unsigned)xcds;
     a.per_xcd = (unsigned)((total + xcds - 1) / xcds);
     int rc = ALCS_E_UNSUPPORTED;
-    if (plan.kind == k128) {
+    constexpr bool kDeep = E != kF32 && !BK;  // (gradients of such shapes take tiles of 64 rows)
+    if (plan.kind == k128 && kDeep && total <= cus && a.ktiles >= 32 * a.splits) {
+        if constexpr (kDeep) rc = launch_mid<E, T, 128, 4, AK, BK, GATED>(a, stream);
+    } else if (plan.kind == k128) {
         rc = launch_mid<E, T, 128, 2, AK, BK, GATED>(a, stream);
     } else if (plan.kind == k64) {
         rc = launch_mid<E, T, 64, 3, AK, BK, GATED>(a, stream);

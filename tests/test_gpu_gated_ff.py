@@ -55,6 +55,13 @@ def test_forward(i, dtype):
         run_forward(X, Wg, Wu, bg, bu, kind, keep, ws, "%s %s %s" % (FORWARD[i], dtype, kind))
 
 
+@pytest.mark.parametrize("T,D,F", [(100, 2056, 16380), (128, 2111, 16300), (256, 4096, 8192)])
+def test_forward_deep(T, D, F):
+    # one workgroup to a compute unit, many K tiles
+    X, Wg, Wu, bg, bu = operands(T, D, F, torch.bfloat16, 4)
+    run_forward(X, Wg, Wu, bg, bu, "silu", True, scratch(alcs.alcs_gated_ff_workspace_bytes(T, D, F, torch.bfloat16)), "deep")
+
+
 @pytest.mark.parametrize("kind", GATES)
 @pytest.mark.parametrize("dtype", TYPES)
 def test_gates_over_their_range(kind, dtype):

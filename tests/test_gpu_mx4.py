@@ -116,6 +116,16 @@ def test_product(i):
         assert intact()
 
 
+@pytest.mark.parametrize("M,N,cols", [(100, 32000, 8100), (256, 16380, 8192)])
+def test_product_deep(M, N, cols):
+    # one workgroup to a compute unit, many K tiles
+    (xc, xs), (wc, ws) = stored(M, cols, 7), stored(N, cols, 8)
+    y, intact = guarded(M, N, dtype=torch.bfloat16)
+    alcs.alcs_mx4_linear(xc, xs, wc, ws, None, y, workspace=workspace(M, N, padded(cols)))
+    check(y, *linear_ref(xc, xs, wc, ws, None, "none"), "deep")
+    assert intact()
+
+
 @pytest.mark.parametrize("M", [3, 40, 150])
 def test_product_of_blocks_that_are_not_finite(M):
     x, w = values(M, 300, 1, std=0.2), values(70, 300, 2, std=0.2)
