@@ -213,6 +213,7 @@ struct BackwardSpace {  // bytes from the start of the workspace
     int pitch;          // of dG and dU, elements
     long long dG, dU, sums, copies, partial, total;
     int parts, rows;
+    Plans plans;
 };
 inline BackwardSpace backward_space(int T, int D, int F, int E, int cus) {
     BackwardSpace s{};
@@ -227,9 +228,9 @@ inline BackwardSpace backward_space(int T, int D, int F, int E, int cus) {
     s.dU = each;
     s.sums = 2 * each;
     s.copies = s.sums + whole256((long long)s.parts * 2 * F * 4);
-    s.partial = s.copies + std::max(2 * copy_bytes(F, D, E), copy_bytes(T, D, E));  // the weights', then X's in their place
-    s.total = s.partial + std::max(plan_tiles(dx_shape(E, T, D, s.pitch), INT64_MAX, cus).workspace,
-                                   plan_tiles(dw_shape(E, T, D, F), INT64_MAX, cus).workspace);
+    s.partial = s.copies + forward_copies(E, T, D, F);
+    s.plans = plan_pair(dx_shape(E, T, D, s.pitch), dw_shape(E, T, D, F), cus);
+    s.total = s.partial + s.plans.workspace;
     return s;
 }
 
@@ -265,35 +266,36 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
     }
     const long long sz = bytes_of(E), pitch = s.pitch * sz;
     const int columns = whole_pieces(b.D, E);
+    Args x{}, w{};
     if (b.dX) {  // dX = dG Wg + dU Wu: one sum over two segments
-        Args a{};
-        a.A[0] = {(const char *)g.dG, pitch, nullptr, b.T};
-        a.A[1] = {(const char *)g.dU, pitch, nullptr, b.T};
-        a.B[0] = {(const char *)b.Wg, b.ldg * sz, nullptr, columns};
-        a.B[1] = {(const char *)b.Wu, b.ldu * sz, nullptr, columns};
-        if ((rc = align_rows<E>({&a.B[0], &a.B[1]}, {b.F, b.F}, b.D, workspace + s.copies, stream)) != ALCS_OK) return rc;
-        a.M = b.T; a.N = b.D; a.KA = s.pitch; a.KB = b.F;
-        a.segs = 2; a.results = 1;
-        a.out[0] = b.dX;
-        a.ldo = b.D;
-        const Plan p = plan_tiles(dx_shape(E, b.T, b.D, s.pitch), INT64_MAX, cus);
-        if ((rc = launch_tiles<E, T, false, true, false>(a, p, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
+        x.A[0] = {(const char *)g.dG, pitch, nullptr, b.T};
+        x.A[1] = {(const char *)g.dU, pitch, nullptr, b.T};
+        x.B[0] = {(const char *)b.Wg, b.ldg * sz, nullptr, columns};
+        x.B[1] = {(const char *)b.Wu, b.ldu * sz, nullptr, columns};
+        x.M = b.T; x.N = b.D; x.KA = s.pitch; x.KB = b.F;
+        x.segs = 2; x.results = 1;
+        x.out[0] = b.dX;
+        x.ldo = b.D;
     }
     if (b.dWg) {  // dWg = dG^T X and dWu = dU^T X
-        Args a{};
-        a.A[0] = {(const char *)g.dG, pitch, nullptr, s.pitch};
-        a.A[1] = {(const char *)g.dU, pitch, nullptr, s.pitch};
-        a.B[0] = {(const char *)b.X, b.ldx * sz, nullptr, columns};
-        if ((rc = align_rows<E>({&a.B[0]}, {b.T}, b.D, workspace + s.copies, stream)) != ALCS_OK) return rc;
-        a.B[1] = a.B[0];
-        a.M = b.F; a.N = b.D; a.KA = a.KB = b.T;
-        a.segs = 1; a.results = 2;
-        a.out[0] = b.dWg; a.out[1] = b.dWu;
-        a.ldo = b.D;
-        const Plan p = plan_tiles(dw_shape(E, b.T, b.D, b.F), INT64_MAX, cus);
-        if ((rc = launch_tiles<E, T, true, true, false>(a, p, workspace + s.partial, cus, xcds, stream)) != ALCS_OK) return rc;
+        w.A[0] = {(const char *)g.dG, pitch, nullptr, s.pitch};
+        w.A[1] = {(const char *)g.dU, pitch, nullptr, s.pitch};
+        w.B[0] = {(const char *)b.X, b.ldx * sz, nullptr, columns};
+        w.M = b.F; w.N = b.D; w.KA = w.KB = b.T;
+        w.segs = 1; w.results = 2;
+        w.out[0] = b.dWg; w.out[1] = b.dWu;
+        w.ldo = b.D;
     }
-    return ALCS_OK;
+    char *copies = workspace + s.copies, *partial = workspace + s.partial;
+    if (b.dX && b.dWg) rc = align_rows<E>({&x.B[0], &x.B[1], &w.B[0]}, {b.F, b.F, b.T}, b.D, copies, stream);
+    else if (b.dX) rc = align_rows<E>({&x.B[0], &x.B[1]}, {b.F, b.F}, b.D, copies, stream);
+    else if (b.dWg) rc = align_rows<E>({&w.B[0]}, {b.T}, b.D, copies, stream);
+    if (rc != ALCS_OK) return rc;
+    w.B[1] = w.B[0];
+    const Shape sx = dx_shape(E, b.T, b.D, s.pitch), sw = dw_shape(E, b.T, b.D, b.F);
+    if (s.plans.together && b.dX && b.dWg) return launch_pair<E, T>(x, w, sx, sw, s.plans, partial, xcds, stream);
+    if (b.dX && (rc = launch_tiles<E, T, false, true, false>(x, plan_tiles(sx, s.plans.workspace, cus), partial, cus, xcds, stream)) != ALCS_OK) return rc;
+    return b.dWg ? launch_tiles<E, T, true, true, false>(w, plan_tiles(sw, s.plans.workspace, cus), partial, cus, xcds, stream) : ALCS_OK;
 }
 
 int check(int T, int D, int F, int dtype, int gate) {

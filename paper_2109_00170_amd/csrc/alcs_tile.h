@@ -443,8 +443,8 @@ __device__ inline void tile_at(const Args &a, unsigned id, int &m, int &n, int &
 }
 // Workgroups are dealt round-robin to the XCDs: numbers are exchanged such that an XCD works on neighbouring tiles and
 // finds their operands in its L2.
-__device__ inline bool tile_of(const Args &a, int &m, int &n, int &z) {
-    const unsigned id = (blockIdx.x % a.xcds) * a.per_xcd + blockIdx.x / a.xcds;
+__device__ inline bool tile_of(const Args &a, unsigned block, int &m, int &n, int &z) {
+    const unsigned id = (block % a.xcds) * a.per_xcd + block / a.xcds;
     if (id >= a.total) return false;
     tile_at(a, id, m, n, z);
     return true;
@@ -626,13 +626,12 @@ template <int E, int BM, int BN, bool AK, bool BK, bool GATED> struct Feed {
 // tiles are no more than the card has units have all of its LDS, and with four K tiles there the weights of a deep product
 // arrive as fast as memory has them: 65 x 4096 -> 2 x 16384 (bfloat16) 44 us (6.2 TB/s), with two 62; 256 x 4096 ->
 // 2 x 8192 39 and 47.  (Of 16 K tiles, 512 x 1024 -> 2 x 4096, two are faster: 13.2 us, four 13.7.)
-template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 2) void k_mid(const Args a) {
+template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __device__ __forceinline__ void mid_tile(const Args &a, unsigned block, char *lds) {
     typedef Feed<E, BM, 128, AK, BK, GATED> Feeds;
     constexpr int FM = BM / 32, FN = 4, kA = Feeds::kA, kB = Feeds::kB, kSA = Feeds::kSA, kBuf = Feeds::kBuf;
     constexpr int kSlots = FM * FN, kReads = FM + FN;
-    extern __shared__ __align__(16) char lds[];
     int tm, tn, z;
-    if (!tile_of(a, tm, tn, z)) return;
+    if (!tile_of(a, block, tm, tn, z)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
     const int result = a.results == 2 ? z & 1 : 0, split = a.results == 2 ? z >> 1 : z;
@@ -719,6 +718,18 @@ template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global
 #pragma unroll
         for (int j = 0; j < FN; ++j) *(v4f *)slab_at(slab, FN * 64, i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[i][j];
     finish_rows<T, GATED, FN * 16>(a, slab, FM * 16, feed.m0 + wm * FM * 16, feed.n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
+}
+template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 2) void k_mid(const Args a) {
+    extern __shared__ __align__(16) char lds[];
+    mid_tile<E, T, BM, NS, AK, BK, GATED>(a, blockIdx.x, lds);
+}
+constexpr int stages_of(int BM) { return BM == 64 ? 3 : 2; }  // of two workgroups on a compute unit
+// A layer's two gradients in one launch, dX (K strided in B) and dW (in both): alone neither fills the card where there
+// are few tiles.  The product whose workgroups take longer is the first; nx, nw: its workgroups, a multiple of the XCDs.
+template <int E, class T, int BMX, int BMW> __global__ __launch_bounds__(256, 2) void k_pair(const Args x, const Args w, unsigned nx, unsigned nw, int x_first) {
+    extern __shared__ __align__(16) char lds[];
+    if (x_first ? blockIdx.x < nx : blockIdx.x >= nw) mid_tile<E, T, BMX, stages_of(BMX), false, true, false>(x, blockIdx.x - (x_first ? 0 : nw), lds);
+    else mid_tile<E, T, BMW, stages_of(BMW), true, true, false>(w, blockIdx.x - (x_first ? nx : 0), lds);
 }
 
 // ------------------------------------------------------------------------------ large tiles
@@ -1029,26 +1040,38 @@ inline Plan plan_of(const Shape &s, int kind, int splits) {
 //   500 x 512 -> 2 x 1365 (float32): 64 rows 23.7 us, 128 x 128 40.2
 //   512 x 8192 -> 1024 (bfloat16): 64 rows in eight parts 30 us, in one 62, 128 x 128 in eight parts 31, 256 x 256 178
 //   2048 x 4096 -> 2 x 4096 (bfloat16): 256 x 256 107 us, 128 x 128 128
-inline double time_of(const Shape &s, const Plan &p, int cus) {
-    struct Cost { double fixed, alone, two; };
+struct Cost { double fixed, alone, two; };
+inline Cost cost_of(const Shape &s, int kind) {
     static const Cost f32[] = {{}, {6, 1.8, 3.6}, {5, 1.0, 1.85}};
     static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}};
     static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}};
-    const Cost &c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[p.kind];
-    const bool strided = s.strided && s.E != kF32 && p.kind != kBig;
-    const double alone = c.alone * (strided ? 1.3 : 1.0), two = c.two * (strided && p.kind == k64 ? 1.07 : 1.0);
+    Cost c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[kind];
+    if (s.strided && s.E == kF32) {
+        if (kind == k128) c.alone *= 1.2;
+    } else if (s.strided && kind != kBig) {
+        c.alone *= 1.3;
+        if (kind == k64) c.two *= 1.07;
+    }
+    return c;
+}
+inline double depth_of(const Shape &s, const Plan &p) { return (double)(long long)(p.ktiles * s.segs / p.splits); }
+inline double join_time(const Plan &p) { return p.splits > 1 ? 4 + (double)p.workspace * 2 / 8e6 : 0; }
+inline double time_of(const Shape &s, const Plan &p, int cus) {
+    const Cost c = cost_of(s, p.kind);
     const long long tiles = (long long)p.tiles_m * p.tiles_n * s.results * p.splits;
-    const double depth = (double)(long long)(p.ktiles * s.segs / p.splits);
+    const double depth = depth_of(s, p);
     double t;
     if (p.kind == kBig) {
         t = c.fixed + (double)up(tiles, cus) * (depth * c.alone + 6);
     } else {
         const long long full = tiles / (2 * cus), left = tiles % (2 * cus);
-        t = c.fixed + (double)full * (depth * two + 2);
-        if (left) t += depth * (left <= cus ? alone : two);
+        t = c.fixed + (double)full * (depth * c.two + 2);
+        if (left) t += depth * (left <= cus ? c.alone : c.two);
     }
-    return p.splits > 1 ? t + 4 + (double)p.workspace * 2 / 8e6 : t;
+    return t + join_time(p);
 }
+// (a launch that joins has less than 2^32 threads, of four sums each)
+inline bool can_split(const Shape &s, const Plan &p) { return p.ktiles * s.segs >= 2 * p.splits && s.results * s.M * s.N < 1LL << 33; }
 // workspace: bytes there are for a split.
 inline Plan plan_tiles(const Shape &s, long long workspace, int cus) {
     Plan best{};
@@ -1057,8 +1080,7 @@ inline Plan plan_tiles(const Shape &s, long long workspace, int cus) {
         if (kind == kBig && s.E == kF32) continue;
         for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
             const Plan p = plan_of(s, kind, splits);
-            // (a launch that joins has less than 2^32 threads, of four sums each)
-            if (splits > 1 && (kind == kBig || p.workspace > workspace || p.ktiles * s.segs < 2 * splits || s.results * s.M * s.N >= 1LL << 33)) break;
+            if (splits > 1 && (kind == kBig || p.workspace > workspace || !can_split(s, p))) break;
             const double t = time_of(s, p, cus);
             if (best.tiles_m == 0 || t < least) { best = p; least = t; }
         }
@@ -1091,9 +1113,8 @@ template <int E, class T, bool AK, bool BK, bool GATED> int launch_big(Args &a, 
     hipLaunchKernelGGL(kern, dim3(std::min(a.per_xcd, share) * a.xcds), dim3(256), lds, stream, a);
     return launched();
 }
-// The product that `a` describes (operands, sizes, outputs and segs / results set; rows aligned and near), by `plan`.
-template <int E, class T, bool AK, bool BK, bool GATED>
-int launch_tiles(Args a, const Plan &plan, void *workspace, int cus, int xcds, hipStream_t stream) {
+// `a`, whose operands, sizes, outputs and segs / results are set (rows aligned and near), gets the rest by `plan`.
+inline int place_tiles(Args &a, const Plan &plan, void *workspace, int xcds) {
     a.tiles_m = plan.tiles_m; a.tiles_n = plan.tiles_n; a.ktiles = plan.ktiles; a.splits = plan.splits;
     if (plan.splits > 1 && !workspace) return ALCS_E_INVALID_ARG;
     a.partial = plan.splits > 1 ? (float *)workspace : nullptr;
@@ -1102,21 +1123,93 @@ int launch_tiles(Args a, const Plan &plan, void *workspace, int cus, int xcds, h
     a.total = (unsigned)total;
     a.xcds = (unsigned)xcds;
     a.per_xcd = (unsigned)((total + xcds - 1) / xcds);
-    int rc = ALCS_E_UNSUPPORTED;
-    constexpr bool kDeep = E != kF32 && !BK;  // (gradients of such shapes take tiles of 64 rows)
-    if (plan.kind == k128 && kDeep && total <= cus && a.ktiles >= 32 * a.splits) {
-        if constexpr (kDeep) rc = launch_mid<E, T, 128, 4, AK, BK, GATED>(a, stream);
-    } else if (plan.kind == k128) {
-        rc = launch_mid<E, T, 128, 2, AK, BK, GATED>(a, stream);
-    } else if (plan.kind == k64) {
-        rc = launch_mid<E, T, 64, 3, AK, BK, GATED>(a, stream);
-    } else {
-        if constexpr (E != kF32) rc = launch_big<E, T, AK, BK, GATED>(a, cus, stream);
-    }
-    if (rc != ALCS_OK || a.splits == 1) return rc;
+    return ALCS_OK;
+}
+template <class T, bool GATED> int launch_join(const Args &a, hipStream_t stream) {
+    if (a.splits == 1) return ALCS_OK;
     const long long quads = (long long)(GATED ? 1 : a.results) * a.M * ((a.N + 3) / 4);
     hipLaunchKernelGGL((k_join<T, GATED>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, a);
     return launched();
+}
+template <int E, class T, bool AK, bool BK, bool GATED>
+int launch_tiles(Args a, const Plan &plan, void *workspace, int cus, int xcds, hipStream_t stream) {
+    int rc = place_tiles(a, plan, workspace, xcds);
+    if (rc != ALCS_OK) return rc;
+    constexpr bool kDeep = E != kF32 && !BK;  // (gradients of such shapes take tiles of 64 rows)
+    if (plan.kind == k128 && kDeep && a.total <= (unsigned)cus && a.ktiles >= 32 * a.splits) {
+        if constexpr (kDeep) rc = launch_mid<E, T, 128, 4, AK, BK, GATED>(a, stream);
+    } else if (plan.kind == k128) {
+        rc = launch_mid<E, T, 128, stages_of(128), AK, BK, GATED>(a, stream);
+    } else if (plan.kind == k64) {
+        rc = launch_mid<E, T, 64, stages_of(64), AK, BK, GATED>(a, stream);
+    } else {
+        if constexpr (E != kF32) rc = launch_big<E, T, AK, BK, GATED>(a, cus, stream);
+    }
+    return rc == ALCS_OK ? launch_join<T, GATED>(a, stream) : rc;
+}
+
+// Both gradients' plans: in one launch where that takes less than one after the other, as it does but for the largest
+// tiles.  T x D, F, one after the other and together, with the sums joined: 500 x 512, 1365 (float32) 50 and 40 us;
+// 333 x 1000, 2730 (bfloat16) 36 and 30; 256 x 512, 2048 18.4 and 12.6; 2048 x 1024, 4096 78 and 71; 2048 x 4096,
+// 4096 237 and 254.
+struct Plans {
+    Plan x, w;
+    bool together;
+    long long workspace;
+};
+inline Plans plan_pair(const Shape &x, const Shape &w, int cus) {
+    Plans best{plan_tiles(x, INT64_MAX, cus), plan_tiles(w, INT64_MAX, cus), false, 0};
+    const long long apart = std::max(best.x.workspace, best.w.workspace);  // (one of them alone may be asked for)
+    best.workspace = apart;
+    double least = 0.97 * (time_of(x, best.x, cus) + time_of(w, best.w, cus) + 4);
+    for (int kx : {k128, k64}) {
+        const Cost cx = cost_of(x, kx);
+        for (int sx : {1, 2, 4, 8, 16}) {
+            const Plan px = plan_of(x, kx, sx);
+            if (sx > 1 && !can_split(x, px)) break;
+            const double dx = depth_of(x, px), nx = (double)px.tiles_m * px.tiles_n * sx;
+            for (int kw : {k128, k64}) {
+                const Cost cw = cost_of(w, kw);
+                for (int sw : {1, 2, 4, 8}) {
+                    const Plan pw = plan_of(w, kw, sw);
+                    if (sw > 1 && !can_split(w, pw)) break;
+                    const double dw = depth_of(w, pw), nw = (double)pw.tiles_m * pw.tiles_n * 2 * sw;
+                    const bool alone = nx + nw <= cus;
+                    const double longx = dx * (alone ? cx.alone : cx.two), longw = dw * (alone ? cw.alone : cw.two);
+                    // all the work shared out (a tenth less than of one kind: short workgroups fill what long ones
+                    // leave), or the longest workgroup
+                    const double shared = 0.9 * (nx * dx * cx.two + nw * dw * cw.two) / 2 / cus + 4 * (nx + nw) / (2 * cus);
+                    const double joins = (sx > 1 ? 2 : 0) + (sw > 1 ? 2 : 0) + (double)(px.workspace + pw.workspace) * 2 / 3e6;
+                    const double t = 6 + std::max(shared, std::max(longx, longw)) + joins;
+                    if (t < least && nx + nw < 1 << 23) {
+                        least = t;
+                        best = {px, pw, true, std::max(apart, whole256(px.workspace) + pw.workspace)};
+                    }
+                }
+            }
+        }
+    }
+    return best;
+}
+template <int E, class T, int BMX, int BMW> int launch_pair_as(const Args &x, const Args &w, bool x_first, hipStream_t stream) {
+    constexpr int lds = std::max(stages_of(BMX) * Feed<E, BMX, 128, false, true, false>::kBuf, stages_of(BMW) * Feed<E, BMW, 128, true, true, false>::kBuf);
+    static_assert(lds <= 80 * 1024, "two workgroups on a compute unit");
+    auto kern = k_pair<E, T, BMX, BMW>;
+    const int rc = allow_lds((const void *)kern, lds);
+    if (rc != ALCS_OK) return rc;
+    const unsigned nx = x.per_xcd * x.xcds, nw = w.per_xcd * w.xcds;
+    hipLaunchKernelGGL(kern, dim3(nx + nw), dim3(256), lds, stream, x, w, nx, nw, (int)x_first);
+    return launched();
+}
+template <int E, class T> int launch_pair(Args x, Args w, const Shape &sx, const Shape &sw, const Plans &p, char *workspace, int xcds, hipStream_t stream) {
+    int rc = place_tiles(x, p.x, workspace, xcds);
+    if (rc == ALCS_OK) rc = place_tiles(w, p.w, workspace + whole256(p.x.workspace), xcds);
+    if (rc != ALCS_OK) return rc;
+    const bool first = depth_of(sx, p.x) * cost_of(sx, p.x.kind).two >= depth_of(sw, p.w) * cost_of(sw, p.w.kind).two;
+    if (p.x.kind == k128) rc = p.w.kind == k128 ? launch_pair_as<E, T, 128, 128>(x, w, first, stream) : launch_pair_as<E, T, 128, 64>(x, w, first, stream);
+    else rc = p.w.kind == k128 ? launch_pair_as<E, T, 64, 128>(x, w, first, stream) : launch_pair_as<E, T, 64, 64>(x, w, first, stream);
+    if (rc == ALCS_OK) rc = launch_join<T, false>(x, stream);
+    return rc == ALCS_OK ? launch_join<T, false>(w, stream) : rc;
 }
 // A few rows of A: k_few's way is the shortest where its workgroups, of 16 columns each, are few; with more, tiles of 64
 // rows stream the weights faster, however few the rows are.  1 x 2048 -> 2 x 8192 (bfloat16): 13.5 us, tiles 15.2;
