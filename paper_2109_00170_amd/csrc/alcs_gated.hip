@@ -74,25 +74,9 @@ template <class T, int AHEAD> __global__ __launch_bounds__(256) void k_gate_grad
         a.sums[((long long)blockIdx.y * 2 + plane) * a.F + n] = s;
     }
 }
-// The parts' sums: 32 columns and eight shares of the parts a workgroup, each added in the order of the parts, the
-// shares in theirs.
-template <class T> __global__ __launch_bounds__(256) void k_bias_grad(const float *sums, int parts, int F, T *dbg, T *dbu) {
-    __shared__ float join[8][32];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const long long at = (long long)blockIdx.x * 32 + x;
-    float s = 0.0f;
-    if (at < 2LL * F) {
-        const int from = (int)((long long)parts * y / 8), to = (int)((long long)parts * (y + 1) / 8);
-#pragma clang loop unroll_count(8)
-        for (int k = from; k < to; ++k) s += sums[(long long)k * 2 * F + at];
-    }
-    join[y][x] = s;
-    __syncthreads();
-    if (y || at >= 2LL * F) return;
-#pragma unroll
-    for (int k = 1; k < 8; ++k) s += join[k][x];
-    T *out = at < F ? dbg : dbu;
-    if (out) out[at % F] = (T)s;
+template <class T> __global__ __launch_bounds__(256) void k_bias_grad(const BiasArgs a) {
+    __shared__ float lds[256];
+    bias_tile<T>(a, blockIdx.x, lds);
 }
 template <class T> __global__ __launch_bounds__(256) void k_fill_zero(T *p, long long n) {
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) p[i] = (T)0.0f;
@@ -259,9 +243,10 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
     auto grad = s.rows == 16 ? k_gate_grad<T, 4> : k_gate_grad<T, 1>;
     hipLaunchKernelGGL(grad, dim3((unsigned)((s.pitch + 255) / 256), (unsigned)s.parts), dim3(256), 0, stream, g);
     if ((rc = launched()) != ALCS_OK) return rc;
-    if (g.sums) {
-        hipLaunchKernelGGL((k_bias_grad<T>), dim3((unsigned)((2LL * b.F + 31) / 32)), dim3(256), 0, stream, g.sums, s.parts, b.F,
-                           (T *)b.dbg, (T *)b.dbu);
+    BiasArgs bias{g.sums, s.parts, b.F, b.dbg, b.dbu, g.sums ? (unsigned)((2LL * b.F + 31) / 32) : 0};
+    const bool together = s.plans.together && b.dX && b.dWg;
+    if (g.sums && !together) {
+        hipLaunchKernelGGL((k_bias_grad<T>), dim3(bias.blocks), dim3(256), 0, stream, bias);
         if ((rc = launched()) != ALCS_OK) return rc;
     }
     const long long sz = bytes_of(E), pitch = s.pitch * sz;
@@ -293,7 +278,7 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
     if (rc != ALCS_OK) return rc;
     w.B[1] = w.B[0];
     const Shape sx = dx_shape(E, b.T, b.D, s.pitch), sw = dw_shape(E, b.T, b.D, b.F);
-    if (s.plans.together && b.dX && b.dWg) return launch_pair<E, T>(x, w, sx, sw, s.plans, partial, xcds, stream);
+    if (together) return launch_pair<E, T>(x, w, bias, sx, sw, s.plans, partial, xcds, stream);
     if (b.dX && (rc = launch_tiles<E, T, false, true, false>(x, plan_tiles(sx, s.plans.workspace, cus), partial, cus, xcds, stream)) != ALCS_OK) return rc;
     return b.dWg ? launch_tiles<E, T, true, true, false>(w, plan_tiles(sw, s.plans.workspace, cus), partial, cus, xcds, stream) : ALCS_OK;
 }

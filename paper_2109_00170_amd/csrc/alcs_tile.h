@@ -724,12 +724,43 @@ template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global
     mid_tile<E, T, BM, NS, AK, BK, GATED>(a, blockIdx.x, lds);
 }
 constexpr int stages_of(int BM) { return BM == 64 ? 3 : 2; }  // of two workgroups on a compute unit
-// A layer's two gradients in one launch, dX (K strided in B) and dW (in both): alone neither fills the card where there
-// are few tiles.  The product whose workgroups take longer is the first; nx, nw: its workgroups, a multiple of the XCDs.
-template <int E, class T, int BMX, int BMW> __global__ __launch_bounds__(256, 2) void k_pair(const Args x, const Args w, unsigned nx, unsigned nw, int x_first) {
+
+// The sums that the gradients at the gate were left in, by parts of the rows: 32 columns and eight shares of the parts a
+// workgroup, each added in the order of the parts, the shares in theirs.
+struct BiasArgs {
+    const float *sums;  // [part][2][F]
+    int parts, F;
+    void *dbg, *dbu;
+    unsigned blocks;
+};
+template <class T> __device__ inline void bias_tile(const BiasArgs &a, unsigned block, float *lds) {
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const long long at = (long long)block * 32 + x;
+    float s = 0.0f;
+    if (at < 2LL * a.F) {
+        const int from = (int)((long long)a.parts * y / 8), to = (int)((long long)a.parts * (y + 1) / 8);
+#pragma clang loop unroll_count(8)
+        for (int k = from; k < to; ++k) s += a.sums[(long long)k * 2 * a.F + at];
+    }
+    lds[y * 32 + x] = s;
+    __syncthreads();
+    if (y || at >= 2LL * a.F) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s += lds[k * 32 + x];
+    T *out = (T *)(at < a.F ? a.dbg : a.dbu);
+    if (out) out[at % a.F] = (T)s;
+}
+
+// A layer's gradients in one launch: dX (K strided in B) and dW (in both), which alone do not fill the card where there
+// are few tiles, and the biases'.  The product whose workgroups take longer is the first; nx, nw: its workgroups, a
+// multiple of the XCDs.
+template <int E, class T, int BMX, int BMW>
+__global__ __launch_bounds__(256, 2) void k_pair(const Args x, const Args w, const BiasArgs b, unsigned nx, unsigned nw, int x_first) {
     extern __shared__ __align__(16) char lds[];
-    if (x_first ? blockIdx.x < nx : blockIdx.x >= nw) mid_tile<E, T, BMX, stages_of(BMX), false, true, false>(x, blockIdx.x - (x_first ? 0 : nw), lds);
-    else mid_tile<E, T, BMW, stages_of(BMW), true, true, false>(w, blockIdx.x - (x_first ? nx : 0), lds);
+    const unsigned block = blockIdx.x;
+    if (block >= nx + nw) bias_tile<T>(b, block - nx - nw, (float *)lds);
+    else if (x_first ? block < nx : block >= nw) mid_tile<E, T, BMX, stages_of(BMX), false, true, false>(x, block - (x_first ? 0 : nw), lds);
+    else mid_tile<E, T, BMW, stages_of(BMW), true, true, false>(w, block - (x_first ? nx : 0), lds);
 }
 
 // ------------------------------------------------------------------------------ large tiles
@@ -1191,23 +1222,23 @@ inline Plans plan_pair(const Shape &x, const Shape &w, int cus) {
     }
     return best;
 }
-template <int E, class T, int BMX, int BMW> int launch_pair_as(const Args &x, const Args &w, bool x_first, hipStream_t stream) {
+template <int E, class T, int BMX, int BMW> int launch_pair_as(const Args &x, const Args &w, const BiasArgs &b, bool x_first, hipStream_t stream) {
     constexpr int lds = std::max(stages_of(BMX) * Feed<E, BMX, 128, false, true, false>::kBuf, stages_of(BMW) * Feed<E, BMW, 128, true, true, false>::kBuf);
     static_assert(lds <= 80 * 1024, "two workgroups on a compute unit");
     auto kern = k_pair<E, T, BMX, BMW>;
     const int rc = allow_lds((const void *)kern, lds);
     if (rc != ALCS_OK) return rc;
     const unsigned nx = x.per_xcd * x.xcds, nw = w.per_xcd * w.xcds;
-    hipLaunchKernelGGL(kern, dim3(nx + nw), dim3(256), lds, stream, x, w, nx, nw, (int)x_first);
+    hipLaunchKernelGGL(kern, dim3(nx + nw + b.blocks), dim3(256), lds, stream, x, w, b, nx, nw, (int)x_first);
     return launched();
 }
-template <int E, class T> int launch_pair(Args x, Args w, const Shape &sx, const Shape &sw, const Plans &p, char *workspace, int xcds, hipStream_t stream) {
+template <int E, class T> int launch_pair(Args x, Args w, const BiasArgs &b, const Shape &sx, const Shape &sw, const Plans &p, char *workspace, int xcds, hipStream_t stream) {
     int rc = place_tiles(x, p.x, workspace, xcds);
     if (rc == ALCS_OK) rc = place_tiles(w, p.w, workspace + whole256(p.x.workspace), xcds);
     if (rc != ALCS_OK) return rc;
     const bool first = depth_of(sx, p.x) * cost_of(sx, p.x.kind).two >= depth_of(sw, p.w) * cost_of(sw, p.w.kind).two;
-    if (p.x.kind == k128) rc = p.w.kind == k128 ? launch_pair_as<E, T, 128, 128>(x, w, first, stream) : launch_pair_as<E, T, 128, 64>(x, w, first, stream);
-    else rc = p.w.kind == k128 ? launch_pair_as<E, T, 64, 128>(x, w, first, stream) : launch_pair_as<E, T, 64, 64>(x, w, first, stream);
+    if (p.x.kind == k128) rc = p.w.kind == k128 ? launch_pair_as<E, T, 128, 128>(x, w, b, first, stream) : launch_pair_as<E, T, 128, 64>(x, w, b, first, stream);
+    else rc = p.w.kind == k128 ? launch_pair_as<E, T, 64, 128>(x, w, b, first, stream) : launch_pair_as<E, T, 64, 64>(x, w, b, first, stream);
     if (rc == ALCS_OK) rc = launch_join<T, false>(x, stream);
     return rc == ALCS_OK ? launch_join<T, false>(w, stream) : rc;
 }
