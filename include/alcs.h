@@ -510,6 +510,8 @@ int alcs_pack_weights_device(const float *W_dev, const uint8_t *mask_dev, int Co
  * instead of pruned (alcs_mx4_*), and two projections with a gate between them as one layer (alcs_gated_ff),
  * with its gradients.  Matrices are row-major with one row per image position, token or output channel;
  * tensors are of one alcs_dtype, 16-bit values are rounded to nearest even, sums are float32 and biases float32.
+ * Tensors need their type's alignment and no more, but for codes, scales and workspaces; infinities and NaN are
+ * treated as said below, and by the sums as arithmetic has it.
  */
 typedef enum alcs_dtype {
     ALCS_F32 = 0,

@@ -33,7 +33,7 @@ template <class T> __device__ inline void load4(const T *p, int n, float v[4]) {
 
 // AHEAD: a thread's rows whose loads are in flight together.
 template <class T, int AHEAD> __global__ __launch_bounds__(256) void k_gate_grad(const GradArgs a) {
-    __shared__ float join[4][64][8];
+    __shared__ float join[4][64][9];  // (8 of them; 9 for the banks)
     const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
     const int c = (blockIdx.x * 64 + x) * 4;
     const int r0 = blockIdx.y * a.rows, r1 = min(r0 + a.rows, a.T);
