@@ -224,7 +224,7 @@ struct BackwardArgs {
     void *dX, *dWg, *dWu, *dbg, *dbu;
     int T, D, F, gate;
 };
-template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus, int xcds, hipStream_t stream) {
+template <int E> int backward_as(const BackwardArgs &b, char *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     typedef typename TypeOf<E>::type T;
     int rc;
     if (b.T == 0) {  // sums over no rows
@@ -234,6 +234,7 @@ template <int E> int backward_as(const BackwardArgs &b, char *workspace, int cus
         return fill_zero<T>(b.dbu, b.F, stream);
     }
     const BackwardSpace s = backward_space(b.T, b.D, b.F, E, cus);
+    if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < s.total) return ALCS_E_INVALID_ARG;
     GradArgs g{};
     g.G = b.G; g.U = b.U; g.dH = b.dH;
     g.dG = workspace + s.dG; g.dU = workspace + s.dU;
@@ -348,12 +349,10 @@ extern "C" int alcs_gated_ff_backward(const void *X_dev, long long ldx, const vo
     if (T > 0 && (!X_dev || !Wg_dev || !Wu_dev || !G_dev || !U_dev || !dH_dev)) return ALCS_E_INVALID_ARG;
     int cus = 0, xcds = 0;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    if (T > 0 && (!workspace_dev || (uintptr_t)workspace_dev % 16 || workspace_bytes < backward_space(T, D, F, dtype, cus).total))
-        return ALCS_E_INVALID_ARG;
     const BackwardArgs b = {X_dev, Wg_dev, Wu_dev, G_dev, U_dev, dH_dev, ldx, ldg, ldu, dX_dev, dWg_dev, dWu_dev, dbg_dev, dbu_dev,
                             T, D, F, gate};
     const hipStream_t st = (hipStream_t)stream;
-    if (dtype == ALCS_F32) return backward_as<kF32>(b, (char *)workspace_dev, cus, xcds, st);
-    if (dtype == ALCS_BF16) return backward_as<kBF16>(b, (char *)workspace_dev, cus, xcds, st);
-    return backward_as<kF16>(b, (char *)workspace_dev, cus, xcds, st);
+    if (dtype == ALCS_F32) return backward_as<kF32>(b, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
+    if (dtype == ALCS_BF16) return backward_as<kBF16>(b, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
+    return backward_as<kF16>(b, (char *)workspace_dev, workspace_bytes, cus, xcds, st);
 }
