@@ -175,7 +175,7 @@ template <int E> int gated_as(Args a, char *workspace, long long workspace_bytes
     const int n = per16(E);
     const bool aligned = D % n == 0 && (uintptr_t)a.A[0].p % 16 == 0 && (uintptr_t)a.B[0].p % 16 == 0 && (uintptr_t)a.B[1].p % 16 == 0 &&
                          a.A[0].pitch % 16 == 0 && a.B[0].pitch % 16 == 0 && a.B[1].pitch % 16 == 0;
-    if (few_rows(a.M, a.N, cus)) return launch_few<E, T, true>(a, aligned, stream);
+    if (few_rows(E, a.M, a.N, D, true, cus)) return launch_few<E, T, true>(a, aligned, stream);
     const long long sz = bytes_of(E);
     const bool near = near_rows(a.A[0].p, a.A[0].pitch / sz, D, E, a.M) && near_rows(a.B[0].p, a.B[0].pitch / sz, D, E, a.N) &&
                       near_rows(a.B[1].p, a.B[1].pitch / sz, D, E, a.N);
@@ -301,7 +301,7 @@ extern "C" long long alcs_gated_ff_workspace_bytes(int T, int D, int F, int dtyp
     const int rc = check(T, D, F, dtype, 0);
     if (rc != ALCS_OK) return rc;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    if (few_rows(T, F, cus)) return 0;
+    if (few_rows(dtype, T, F, D, true, cus)) return 0;
     return (D % per16(dtype) ? forward_copies(dtype, T, D, F) : 0) + plan_tiles(forward_shape(dtype, T, whole_pieces(D, dtype), F), INT64_MAX, cus).workspace;
 }
 extern "C" long long alcs_gated_ff_backward_workspace_bytes(int T, int D, int F, int dtype) {

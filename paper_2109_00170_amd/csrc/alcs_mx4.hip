@@ -94,7 +94,7 @@ constexpr int kMaxSize = 1 << 26;
 inline Shape linear_shape(int M, int N, int K) { return {kMX4, false, false, M, N, K, 1, 1}; }
 
 template <class T> int linear_as(const Args &a, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
-    if (few_rows(a.M, a.N, cus)) return launch_few<kMX4, T, false>(a, true, stream);
+    if (few_rows(kMX4, a.M, a.N, a.KA, false, cus)) return launch_few<kMX4, T, false>(a, true, stream);
     const Plan p = plan_tiles(linear_shape(a.M, a.N, a.KA), workspace ? workspace_bytes : 0, cus);
     return launch_tiles<kMX4, T, false, false, false>(a, p, workspace, cus, xcds, stream);
 }
@@ -154,7 +154,7 @@ extern "C" long long alcs_mx4_linear_workspace_bytes(int M, int N, int K) {
     if (rc != ALCS_OK) return rc;
     int cus = 0, xcds = 0;
     if (current_device_shape(&cus, &xcds) != ALCS_OK) return ALCS_E_HIP;
-    return few_rows(M, N, cus) ? 0 : plan_tiles(linear_shape(M, N, K), INT64_MAX, cus).workspace;
+    return few_rows(kMX4, M, N, K, false, cus) ? 0 : plan_tiles(linear_shape(M, N, K), INT64_MAX, cus).workspace;
 }
 
 extern "C" int alcs_mx4_linear(const uint8_t *X_codes_dev, const uint8_t *X_scales_dev, const uint8_t *W_codes_dev,

@@ -1242,11 +1242,25 @@ template <int E, class T> int launch_pair(Args x, Args w, const BiasArgs &b, con
     if (rc == ALCS_OK) rc = launch_join<T, false>(x, stream);
     return rc == ALCS_OK ? launch_join<T, false>(w, stream) : rc;
 }
-// A few rows of A: k_few's way is the shortest where its workgroups, of 16 columns each, are few; with more, tiles of 64
-// rows stream the weights faster, however few the rows are.  1 x 2048 -> 2 x 8192 (bfloat16): 13.5 us, tiles 15.2;
-// 1 x 4096 -> 2 x 16384: 47 us, tiles 43 (6.3 TB/s); 64 x 1000 -> 2 x 2728: 7.4, tiles 12; 64 x 2048 -> 2 x 8192: 28,
-// tiles 15.3; 1 x 8192 -> 16384 (4-bit): 20.5, tiles 17.3.
-inline bool few_rows(int M, int N, int cus) { return M <= 64 && up(N, 16) <= (M <= 16 ? 2 : 1) * cus; }
+// A few rows of A: k_few's way is the shortest while the weights are not much (each of its wavefronts waits for its own
+// loads; tiles have more of them in flight), and the less so the more rows multiply each of them.  Its workgroups have 16
+// columns: many of them start slowly, and few, of long rows, leave compute units idle.  float32 tiles multiply 64 rows at a
+// sixteenth of the 16-bit rate however few there are, and odd rows are copied for them first.  In us, k_few and tiles:
+//   bfloat16   1 x 2048 -> 2 x 8192 (67 MB) 13.2, 15.1; 16 rows 15.6, 15.4; 16 x 4096 -> 2 x 8192 29.0, 25.5; 32 x 2048 ->
+//              2 x 4096 10.8, 11.4; 64 x 2048 -> 2 x 4096 15.1, 13.1; 64 x 1000 -> 2 x 2728 7.1, 9.5;
+//              16 x 8192 -> 2 x 2048 23.9, 16.1; 16 x 512 -> 2 x 16384 8.5, 6.8
+//   float32    16 x 4096 -> 2 x 8192 58, 74; 32 rows 92, 74; 32 x 2048 -> 2 x 4096 24.7, 25.5; 64 x 2047 -> 2 x 4096 42, 48
+//   four bits  1 x 8192 -> 8192 8.9, 11.7; 16384 20.6, 16.6; 16 x 4096 -> 11008 9.2, 13.0; 32 x 8192 -> 8192 22.6, 12.8
+inline bool few_rows(int E, int M, int N, int K, bool gated, int cus) {
+    static const int f32[] = {540, 68, 20}, b16[] = {68, 34, 12}, mx4[] = {36, 18, 9};  // MB of weights for 16, 32, 64 rows
+    if (M > 64) return false;
+    const long long row = E == kMX4 ? K / 2 : (long long)K * bytes_of(E);
+    const int most = (E == kF32 ? f32 : E == kMX4 ? mx4 : b16)[M <= 16 ? 0 : M <= 32 ? 1 : 2];
+    if (E == kF32 && K % per16(E)) return true;  // 64 x 4095 -> 2 x 8191 156, 184
+    if (E != kF32 && (row > 8192 || up(N, 16) > (M > 16 ? 1 : E == kMX4 ? 3 : 2) * cus)) return false;
+    const bool odd = K % per16(E) != 0;  // 1 x 4095 -> 2 x 8191 (bfloat16) 58, 70; 16 rows 78, 74
+    return (gated ? 2 : 1) * row * N <= (odd && M <= 16 ? 2 : 1) * most * 1000000LL;
+}
 template <int E, class T, bool GATED, bool ALIGNED> int launch_few_as(const Args &a, hipStream_t stream) {
     const int pieces = (a.KA + 16 * per16(E) - 1) / (16 * per16(E)), W = std::max(1, std::min(8, pieces));
     const int MF = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4, lds = W * (GATED ? 2 : 1) * MF * 1024;
