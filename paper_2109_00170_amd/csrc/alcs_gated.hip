@@ -1,5 +1,6 @@
 // The gated feed-forward block and its gradients (alcs.h): the two projections, the gate and the product in one
-// kernel, alcs_tile.h's; the backward pass is one pass over [T, F] and two launches of the same kernel.
+// kernel, alcs_tile.h's; the backward pass is one pass over [T, F] and the products behind it, in one launch or
+// two.
 #include "alcs_tile.h"
 
 namespace alcs {
