@@ -491,8 +491,8 @@ template <int E, int R, bool KSTRIDED> struct NearStage {
         if (WHOLE) {
             if (i % 4 == 0) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]), "s"(base), "s"(at) : "memory");
             else if (i % 4 == 1) asm volatile("global_load_lds_dwordx4 %0, %1 offset:1024" ::"v"(off[i]), "s"(base) : "memory");
-            else if (i % 4 == 2) asm volatile("global_load_lds_dwordx4 %0, %1 offset:2048" ::"v"(off[i]), "s"(base) : "memory");
-            else asm volatile("global_load_lds_dwordx4 %0, %1 offset:3072" ::"v"(off[i]), "s"(base) : "memory");
+            else if (i % 4 == 2) asm volatile("global_load_lds_dwordx4 %0, %1 offset:2*1024" ::"v"(off[i]), "s"(base) : "memory");
+            else asm volatile("global_load_lds_dwordx4 %0, %1 offset:3*1024" ::"v"(off[i]), "s"(base) : "memory");
         } else {
             int row, k, l = lane;
             unsigned o = off[i];
