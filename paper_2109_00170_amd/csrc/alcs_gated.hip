@@ -101,7 +101,6 @@ inline bool near_rows(const void *p, long long ld, int columns, int E, int rows)
     const int n = per16(E);
     return (uintptr_t)p % 16 == 0 && columns % n == 0 && (rows <= 1 || (ld % n == 0 && ld * bytes_of(E) <= kNearPitch));
 }
-inline int whole_pieces(int columns, int E) { return (columns + per16(E) - 1) / per16(E) * per16(E); }
 
 // Copies of up to three matrices whose rows the tiles do not take, padded with zeros to whole pieces: a wavefront a row.
 // 2000 x 999 -> 2 x 2731 (bfloat16) 41 + 9 us, where tiles that read odd rows themselves, through registers,
@@ -164,9 +163,6 @@ template <int E> int align_rows(std::initializer_list<Operand *> operands, std::
     return launched();
 }
 
-inline Shape forward_shape(int E, int T, int D, int F) { return {E, true, false, T, F, D, 1, 1}; }
-inline Shape dx_shape(int E, int T, int D, int pitch) { return {E, false, true, T, D, pitch, 2, 1}; }
-inline Shape dw_shape(int E, int T, int D, int F) { return {E, false, true, F, D, T, 1, 2}; }
 inline long long copy_bytes(int rows, int D, int E) { return whole256((long long)rows * whole_pieces(D, E) * bytes_of(E)); }
 inline long long forward_copies(int E, int T, int D, int F) { return copy_bytes(T, D, E) + 2 * copy_bytes(F, D, E); }
 

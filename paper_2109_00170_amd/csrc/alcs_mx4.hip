@@ -91,8 +91,6 @@ inline int check_stored(const void *codes, const void *scales) {
 }
 constexpr int kMaxSize = 1 << 26;
 
-inline Shape linear_shape(int M, int N, int K) { return {kMX4, false, false, M, N, K, 1, 1}; }
-
 template <class T> int linear_as(const Args &a, void *workspace, long long workspace_bytes, int cus, int xcds, hipStream_t stream) {
     if (few_rows(kMX4, a.M, a.N, a.KA, false, cus)) return launch_few<kMX4, T, false>(a, true, stream);
     const Plan p = plan_tiles(linear_shape(a.M, a.N, a.KA), workspace ? workspace_bytes : 0, cus);
