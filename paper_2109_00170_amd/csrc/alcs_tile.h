@@ -129,7 +129,7 @@ template <bool EXACT> __device__ inline void gate_both(int gate, float g, float 
             d = s + g * (s * (1.0f - s)) * 2.0f * kGeluA * (1.0f + 3.0f * kGeluB * b);
             break;
         }
-        case ALCS_GATE_SIGMOID: { const float s = sigmoid<EXACT>(g); v = s; d = s * (1.0f - s); break; }
+        case ALCS_GATE_SIGMOID: v = sigmoid<EXACT>(g); d = v * sigmoid<EXACT>(-g); break;  // (1 - s has no digits left for large g)
         default: v = g; d = 1.0f;
     }
 }

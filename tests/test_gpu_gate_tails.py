@@ -63,7 +63,7 @@ def test_values(kind, dtype, T):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("kind", ["gelu"])
+@pytest.mark.parametrize("kind", ["gelu", "sigmoid"])
 def test_slopes(kind, dtype):
     # one row and one column, so that dWg is dG = dH U gate'(G) and dWu is dU = dH gate(G)
     F = 501
