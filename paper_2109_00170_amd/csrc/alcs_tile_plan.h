@@ -51,9 +51,10 @@ inline Plan plan_of(const Shape &s, int kind, int splits) {
 // alone: 0.32 and 0.50; where the sum runs over rows (transposing reads) a third more; 256 x 256 tiles run at the
 // card's power limit.  A split costs another launch and the sums' way out and back at 8 TB/s (they
 // stay in the last cache).
-//   333 x 1000 -> 2 x 2728 (bfloat16): 128 x 128 tiles 13.7 us, 64 rows 15.0 (258 tiles), 128 x 128 in three parts 22
+//   333 x 1000 -> 2 x 2728 (bfloat16): 128 x 128 tiles 12.5 us, 64 rows 14.3 (258 tiles), 128 x 128 in three parts 22
+//   1000 x 1000 -> 2 x 4096 (bfloat16): 128 x 128 tiles 23.5 us, 64 rows 29.8; 333 x 1024 -> 2 x 2730 11.9 and 11.7
 //   500 x 512 -> 2 x 1365 (float32): 64 rows 23.7 us, 128 x 128 40.2
-//   512 x 8192 -> 1024 (bfloat16): 64 rows in eight parts 30 us, in one 62, 128 x 128 in eight parts 31, 256 x 256 178
+//   dX of 512 x 1024, 4096 (bfloat16): 64 rows in four parts 24 us, in eight 23, in one 54, 128 x 128 in eight 24, 256 x 256 163
 //   2048 x 4096 -> 2 x 4096 (bfloat16): 256 x 256 107 us, 128 x 128 128
 struct Cost { double fixed, alone, two; };
 inline Cost cost_of(const Shape &s, int kind) {
@@ -61,6 +62,9 @@ inline Cost cost_of(const Shape &s, int kind) {
     static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}};
     static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}};
     Cost c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[kind];
+    // rows of 16 bits that do not start at 64 bytes, each 128 bytes of which lie in one line more: two workgroups of 64 rows, which
+    // have the fewest bytes in flight for each they multiply, wait for them
+    if (!s.strided && s.E != kF32 && s.E != kMX4 && s.K * bytes_of(s.E) % 64 && kind == k64) c.two = 0.65;
     if (s.strided && s.E == kF32) {
         if (kind == k128) c.alone *= 1.2;
     } else if (s.strided && kind != kBig) {

@@ -1,4 +1,5 @@
 """The feed-forward products' choice of kernels (csrc/alcs_tile_plan.h), asked for the 256 compute units of an MI355X."""
+import pytest
 import torch
 
 from test_gpu_large_tiles import DW, DX, FORWARD, LINEAR
@@ -26,3 +27,33 @@ def test_sizes_of_the_middle_and_few_rows():
     # without room for the sums K is not shared out
     assert forward_plan(100, 4104, 24, BF).splits > 1 and forward_plan(100, 4104, 24, BF, workspace=0).splits == 1
     assert linear_plan(65, 129, 640).splits == 1 and linear_plan(100, 200, 4096).splits > 1
+
+
+F32 = torch.float32
+MEASURED = [  # T, D, F, type: the fastest of the kernels that were timed for a product of these sizes
+    (333, 1000, 2728, BF, "128"), (333, 1000, 2730, torch.float16, "128"), (333, 1000, 2560, BF, "64"), (333, 1000, 3400, BF, "128"),
+    (333, 1000, 4096, BF, "128"), (333, 1000, 5440, BF, "128"), (200, 1000, 4096, BF, "64"), (200, 1000, 4224, BF, "128"),
+    (250, 1024, 4100, BF, "64"), (130, 1024, 5500, BF, "64"), (100, 2048, 8200, BF, "128"), (384, 512, 2816, BF, "64"),
+    (500, 1000, 2200, BF, "128"), (500, 2000, 2200, BF, "128"), (700, 1000, 4096, BF, "128"), (1000, 1000, 4096, BF, "128"),
+    (1000, 1024, 4096, BF, "128"), (333, 488, 2730, BF, "128"), (333, 512, 2730, BF, "64"), (500, 512, 1365, F32, "64"),
+    (65, 4096, 16384, BF, "128"), (2048, 4096, 4096, BF, "256"),
+    (64, 1000, 2728, BF, "few"), (32, 2048, 4096, BF, "few"), (64, 2048, 4096, BF, "64"), (16, 4096, 8192, BF, "64"),
+    (16, 8192, 2048, BF, "64"), (16, 512, 16384, BF, "64"), (16, 4096, 8192, F32, "few"), (32, 4096, 8192, F32, "64"),
+    (64, 2047, 4096, F32, "few"), (64, 4095, 8191, F32, "few"), (1, 4095, 8191, BF, "few")]
+
+
+@pytest.mark.parametrize("T,D,F,dtype,kind", MEASURED)
+def test_choices_that_were_measured(T, D, F, dtype, kind):
+    assert forward_plan(T, D, F, dtype, workspace=0).kind == kind
+
+
+def test_gradients_together_where_that_was_faster():
+    for T, D, F, dtype, together in ((500, 512, 1365, F32, True), (333, 1000, 2730, BF, True), (256, 512, 2048, BF, True),
+                                     (2048, 1024, 4096, BF, True), (2048, 4096, 4096, BF, False)):
+        assert backward_plan(T, D, F, dtype).together == together
+    assert backward_plan(512, 1024, 4096, BF).dX_alone[:2] in (("64", 4), ("64", 8))
+
+
+@pytest.mark.parametrize("M,N,K,kind", [(1, 8192, 8192, "few"), (1, 16384, 8192, "64"), (16, 11008, 4096, "few"), (32, 8192, 8192, "64")])
+def test_four_bit_choices_that_were_measured(M, N, K, kind):
+    assert linear_plan(M, N, K).kind == kind
