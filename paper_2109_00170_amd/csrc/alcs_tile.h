@@ -385,11 +385,11 @@ template <class T> __device__ inline void finish_gated(const Args &a, long long 
 // than the rest of it.
 __device__ inline char *slab_at(char *slab, int pitch, int row, int piece) { return slab + row * pitch + ((piece ^ (row & 7)) << 4); }
 
-template <class T, bool GATED, int COLS>
+template <class T, bool GATED, int COLS, bool SUMS>  // SUMS: K may be shared out
 __device__ inline void finish_rows(const Args &a, char *slab, int rows, int m0, int n0, int result, int split, int lane) {
     constexpr bool kExact = sizeof(T) == 4;
     constexpr int kOut = GATED ? COLS / 2 : COLS, kPitch = COLS * 4;
-    if (a.partial) {  // four neighbours a lane
+    if (SUMS && a.partial) {  // four neighbours a lane
         constexpr int kLanes = COLS / 4;
         const int piece = lane % kLanes, plane = GATED && piece >= kLanes / 2;
         const int n = n0 + piece % (kOut / 4) * 4, left = a.N - n;
@@ -736,7 +736,7 @@ template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __device
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) *(v4f *)slab_at(slab, FN * 64, i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[i][j];
-    finish_rows<T, GATED, FN * 16>(a, slab, FM * 16, feed.m0 + wm * FM * 16, feed.n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
+    finish_rows<T, GATED, FN * 16, true>(a, slab, FM * 16, feed.m0 + wm * FM * 16, feed.n0 + wn * (GATED ? FN / 2 : FN) * 16, result, split, lane);
 }
 template <int E, class T, int BM, int NS, bool AK, bool BK, bool GATED> __global__ __launch_bounds__(256, 2) void k_mid(const Args a) {
     extern __shared__ __align__(16) char lds[];
@@ -928,7 +928,7 @@ template <int E, class T, bool AK, bool BK, bool GATED> __global__ __launch_boun
                     *(v4f *)slab_at(slab, 512, row, j * 4 + (l >> 4)) = read_at<(decltype(which_quarter)::value * 2 + i) * 8 + j>();
                 });
             });
-            finish_rows<T, GATED, 128>(a, slab, 32, m + quarter * 32, n, which, 0, l);
+            finish_rows<T, GATED, 128, false>(a, slab, 32, m + quarter * 32, n, which, 0, l);
         }
         if (!more) break;
         __syncthreads();
