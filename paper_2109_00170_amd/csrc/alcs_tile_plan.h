@@ -50,26 +50,24 @@ inline Plan plan_of(const Shape &s, int kind, int splits) {
 // for a K tile of 128 bytes a row, of one workgroup alone on its compute unit and of two.  Small tiles of 16 bits
 // alone: 0.32 and 0.50; where the sum runs over rows (transposing reads) a third more; 256 x 256 tiles run at the
 // card's power limit.  A split costs another launch and the sums' way out and back at 8 TB/s (they
-// stay in the last cache).
-//   333 x 1000 -> 2 x 2728 (bfloat16): 128 x 128 tiles 12.5 us, 64 rows 14.3 (258 tiles), 128 x 128 in three parts 22
-//   1000 x 1000 -> 2 x 4096 (bfloat16): 128 x 128 tiles 23.5 us, 64 rows 29.8; 333 x 1024 -> 2 x 2730 11.9 and 11.7
+// stay in the last cache, where the operands were too for the first three lines: as a layer finds them behind others).
+//   333 x 1000 -> 2 x 2730 (bfloat16): 64 rows (258 tiles) 14.5 us, 128 x 128 16.9; from memory 16.9 and 21.8, from L2 15.0 and 13.2
+//   500 x 2000 -> 2 x 2200 (bfloat16): 64 rows (280 tiles) 26.5 us, 128 x 128 23.1
+//   700 x 1024 -> 2 x 4096 (bfloat16): 64 rows (704 tiles) 20.3 us, 128 x 128 18.4; 1000 x 1000 -> 2 x 4096 (1024) 30.5 and 24.3
 //   500 x 512 -> 2 x 1365 (float32): 64 rows 23.7 us, 128 x 128 40.2
 //   dX of 512 x 1024, 4096 (bfloat16): 64 rows in four parts 24 us, in eight 23, in one 54, 128 x 128 in eight 24, 256 x 256 163
 //   2048 x 4096 -> 2 x 4096 (bfloat16): 256 x 256 107 us, 128 x 128 128
-struct Cost { double fixed, alone, two; };
+struct Cost { double fixed, alone, two, round; };  // round: of two, where more tiles follow
 inline Cost cost_of(const Shape &s, int kind) {
-    static const Cost f32[] = {{}, {6, 1.8, 3.6}, {5, 1.0, 1.85}};
-    static const Cost b16[] = {{7, 1.5, 0}, {6, 0.50, 0.97}, {5, 0.32, 0.56}};
-    static const Cost mx4[] = {{7, 1.6, 0}, {6, 0.75, 1.4}, {5, 0.50, 0.90}};
+    static const Cost f32[] = {{}, {6, 1.8, 3.6, 3.6}, {5, 1.0, 1.85, 1.85}};
+    static const Cost b16[] = {{7, 1.5}, {6, 0.50, 0.97, 0.97}, {5, 0.32, 0.56, 0.65}};
+    static const Cost mx4[] = {{7, 1.6}, {6, 0.75, 1.4, 1.4}, {5, 0.50, 0.90, 0.90}};
     Cost c = (s.E == kF32 ? f32 : s.E == kMX4 ? mx4 : b16)[kind];
-    // rows of 16 bits that do not start at 64 bytes, each 128 bytes of which lie in one line more: two workgroups of 64 rows, which
-    // have the fewest bytes in flight for each they multiply, wait for them
-    if (!s.strided && s.E != kF32 && s.E != kMX4 && s.K * bytes_of(s.E) % 64 && kind == k64) c.two = 0.65;
     if (s.strided && s.E == kF32) {
         if (kind == k128) c.alone *= 1.2;
     } else if (s.strided && kind != kBig) {
         c.alone *= 1.3;
-        if (kind == k64) c.two *= 1.07;
+        if (kind == k64) c.round = c.two *= 1.07;
     }
     return c;
 }
@@ -84,7 +82,7 @@ inline double time_of(const Shape &s, const Plan &p, int cus) {
         t = c.fixed + (double)up(tiles, cus) * (depth * c.alone + 6);
     } else {
         const long long full = tiles / (2 * cus), left = tiles % (2 * cus);
-        t = c.fixed + (double)full * (depth * c.two + 2);
+        t = c.fixed + (double)full * (depth * c.round + 2);
         if (left) t += depth * (left <= cus ? c.alone : c.two);
     }
     return t + join_time(p);

@@ -30,12 +30,14 @@ def test_sizes_of_the_middle_and_few_rows():
 
 
 F32 = torch.float32
-MEASURED = [  # T, D, F, type: the fastest of the kernels that were timed for a product of these sizes
-    (333, 1000, 2728, BF, "128"), (333, 1000, 2730, torch.float16, "128"), (333, 1000, 2560, BF, "64"), (333, 1000, 3400, BF, "128"),
-    (333, 1000, 4096, BF, "128"), (333, 1000, 5440, BF, "128"), (200, 1000, 4096, BF, "64"), (200, 1000, 4224, BF, "128"),
-    (250, 1024, 4100, BF, "64"), (130, 1024, 5500, BF, "64"), (100, 2048, 8200, BF, "128"), (384, 512, 2816, BF, "64"),
-    (500, 1000, 2200, BF, "128"), (500, 2000, 2200, BF, "128"), (700, 1000, 4096, BF, "128"), (1000, 1000, 4096, BF, "128"),
-    (1000, 1024, 4096, BF, "128"), (333, 488, 2730, BF, "128"), (333, 512, 2730, BF, "64"), (500, 512, 1365, F32, "64"),
+MEASURED = [  # T, D, F, type: the fastest of the kernels that were timed for a product of these sizes, operands in the last cache
+    (333, 1000, 2730, BF, "64"), (333, 1000, 2730, torch.float16, "64"), (333, 1024, 2730, BF, "64"), (333, 1000, 3400, BF, "64"),
+    (333, 1000, 4096, BF, "64"), (333, 1000, 5440, BF, "64"), (250, 1024, 4100, BF, "64"), (500, 1000, 2200, BF, "64"),
+    (500, 2000, 2200, BF, "128"), (333, 488, 2730, BF, "64"), (333, 512, 2730, BF, "64"), (700, 1000, 4096, BF, "128"),
+    (700, 1024, 4096, BF, "128"), (1000, 1000, 4096, BF, "128"), (1000, 1024, 4096, BF, "128"), (600, 1024, 4096, BF, "128"),
+    (520, 2048, 4096, BF, "128"), (400, 512, 6000, BF, "128"), (512, 1000, 4224, BF, "128"), (300, 1000, 7000, BF, "128"),
+    (1500, 512, 3000, BF, "128"), (100, 1000, 17000, BF, "128"), (700, 2048, 4096, BF, "128"), (900, 1000, 3000, BF, "128"),
+    (520, 512, 4096, BF, "128"), (500, 512, 1365, F32, "64"),
     (65, 4096, 16384, BF, "128"), (2048, 4096, 4096, BF, "256"),
     (64, 1000, 2728, BF, "few"), (32, 2048, 4096, BF, "few"), (64, 2048, 4096, BF, "64"), (16, 4096, 8192, BF, "64"),
     (16, 8192, 2048, BF, "64"), (16, 512, 16384, BF, "64"), (16, 4096, 8192, F32, "few"), (32, 4096, 8192, F32, "64"),
