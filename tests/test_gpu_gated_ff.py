@@ -37,9 +37,8 @@ def run_forward(X, Wg, Wu, bg, bu, kind, keep, ws, what):
     return H
 
 
-# the forms for few rows and their borders, tiles of 128 (K shared out where a workspace is given), tiles of 256 (one and several
-# to a workgroup);
-# sizes that are whole 16-byte pieces and sizes that are not
+# the forms for few rows and their borders, tiles of 64 and 128 rows (K shared out where a workspace is given; several tiles to a
+# compute unit); sizes that are whole 16-byte pieces and sizes that are not
 FORWARD = [(1, 1, 1), (1, 64, 64), (1, 8200, 24), (2, 9, 17), (16, 128, 40), (17, 131, 33), (33, 64, 66), (64, 520, 48),
            (65, 96, 70), (70, 31, 9), (100, 4104, 24), (100, 4101, 23), (129, 200, 257), (300, 1000, 520), (2048, 72, 2048),
            (2100, 136, 2052), (4097, 72, 4100)]

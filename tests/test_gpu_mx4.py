@@ -96,7 +96,7 @@ def workspace(M, N, K):
     return torch.empty(alcs.alcs_mx4_linear_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
 
 
-# rows: a token, all forms for few rows and their borders, tiles of 128 (with K shared out) and of 256
+# rows: a token, all forms for few rows and their borders, tiles of 64 and 128 rows (with K shared out)
 SIZES = [(1, 1, 1), (1, 1000, 2048), (2, 17, 129), (16, 64, 512), (17, 33, 600), (33, 15, 128), (64, 130, 1100), (65, 1, 128),
          (65, 129, 640), (128, 128, 256), (200, 257, 4100), (129, 500, 384), (300, 1000, 1000), (2900, 2901, 390), (2817, 2817, 256),
          (5000, 4999, 300), (4500, 5120, 128)]
