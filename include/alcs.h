@@ -506,9 +506,11 @@ int alcs_pack_weights_device(const float *W_dev, const uint8_t *mask_dev, int Co
                              const alcs_options *options, void *stream, alcs_packed_t **out);
 
 /*
- * Feed-forward layers.  Pointwise and fully connected layers beside the sparse ones above: held in four bits
+ * Feed-forward layers.  Fully connected layers beside the sparse ones above: held in four bits
  * instead of pruned (alcs_mx4_*), and two projections with a gate between them as one layer (alcs_gated_ff),
- * with its gradients.  Matrices are row-major with one row per image position, token or output channel;
+ * with its gradients.  Matrices are row-major with one row per token, image or output channel, the columns next to each
+ * other (images of several positions, whose channels lie apart in the layout of the calls above, have to be
+ * transposed first);
  * tensors are of one alcs_dtype, 16-bit values are rounded to nearest even, sums are float32 and biases float32.
  * Tensors need their type's alignment and no more, but for codes, scales and workspaces; infinities and NaN are
  * treated as said below, and by the sums as arithmetic has it.
@@ -573,8 +575,8 @@ typedef enum alcs_gate {
 } alcs_gate;
 
 /*
- * The gated feed-forward block in one kernel, like the block of alcs_dw_sparse_conv_fused two layers of which
- * the intermediates need not be written out:
+ * The gated feed-forward block, like the block of alcs_dw_sparse_conv_fused two layers of which the intermediates need
+ * not be written out: one launch, one more where a workspace lets K be shared out, one more where operands are copied.
  *   G = X Wg^T + bg,  U = X Wu^T + bu,  H = gate(G) * U  (element by element)
  *   X_dev [T, D], Wg_dev and Wu_dev [F, D] of `dtype`, rows ldx, ldg and ldu elements apart (any pitch >= 0: the
  *   halves or the alternate rows of one tensor will do); bg_dev, bu_dev [F] float32 or NULL; H_dev [T, F], fully

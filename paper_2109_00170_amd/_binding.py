@@ -687,6 +687,9 @@ def alcs_mx4_linear(X_codes, X_scales, W_codes, W_scales, bias, Y, activation=No
 
 
 def alcs_gated_ff_workspace_bytes(T: int, D: int, F: int, dtype) -> int:
+    """What alcs_gated_ff can use on the current GPU for packed tensors.  Views that start at other than 16-byte addresses, or
+    whose rows lie an odd distance or more than 4 MB apart, need (T + 2 F) (D + 8) elements and 1024 bytes more: without
+    them a call of more than 64 rows still gives the results, but several times slower."""
     return _workspace_bytes("alcs_gated_ff_workspace_bytes", T, D, F, _dtype_code(dtype))
 
 
@@ -698,6 +701,7 @@ def alcs_gated_ff(X, Wg, Wu, bg, bu, H, gate="silu", G=None, U=None, workspace=N
 
 
 def alcs_gated_ff_backward_workspace_bytes(T: int, D: int, F: int, dtype) -> int:
+    """What alcs_gated_ff_backward needs on the current GPU, room for copies of any views among its operands included."""
     return _workspace_bytes("alcs_gated_ff_backward_workspace_bytes", T, D, F, _dtype_code(dtype))
 
 

@@ -9,7 +9,7 @@
 //
 // Operands are brought into LDS by the load that writes there directly (16 bytes a lane, a wavefront's 1024
 // bytes in lane order), so the arrangement against bank conflicts is made on the global side: which piece a
-// lane fetches.  Two or three K tiles are in LDS: while one is multiplied, the others are on their way.
+// lane fetches.  Two to four K tiles are in LDS: while one is multiplied, the others are on their way.
 //
 // Layouts.  "K contiguous" (rows of A and B as a linear layer has them): [row][128 bytes], the 16-byte
 // piece c of row r at position c ^ (r & 7).  "K strided" (the operands of a gradient, whose sum runs over
@@ -35,7 +35,6 @@
 namespace alcs {
 namespace tile {
 
-
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef int v8i __attribute__((ext_vector_type(8)));
@@ -54,7 +53,8 @@ template <> struct TypeOf<kBF16> { typedef __bf16 type; };
 template <> struct TypeOf<kF16> { typedef _Float16 type; };
 
 // The gates of alcs.h (alcs_gate).  EXACT: float32 tensors get the library's exponential and division;
-// for results of 16 bits the hardware's exp2 and reciprocal (relative error about 2^-22) are far below the rounding.
+// for results of 16 bits the hardware's exp2 and reciprocal are far below the rounding: relative error about (4 + |g|) 2^-24, since
+// the exponent's rounding grows with it.
 template <bool EXACT> __device__ inline float sigmoid(float g) {
     if (EXACT) return 1.0f / (1.0f + expf(-g));
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
