@@ -157,7 +157,9 @@ inline Plans plan_pair(const Shape &x, const Shape &w, int cus) {
 // A few rows of A: k_few's way is the shortest while the weights are not much (each of its wavefronts waits for its own
 // loads; tiles have more of them in flight), and the less so the more rows multiply each of them.  Its workgroups have 16
 // columns: many of them start slowly, and few, of long rows, leave compute units idle.  float32 tiles multiply 64 rows at a
-// sixteenth of the 16-bit rate however few there are, and odd rows are copied for them first.  In us, k_few and tiles:
+// sixteenth of the 16-bit rate however few there are, and odd rows are copied for them first.  In us, k_few and tiles, one set of
+// operands over and over (with others in between tiles gain where rows are more than a few: bfloat16, 32 x 2048 -> 2 x 4096 14.8, 12.0;
+// 16 x 2048 -> 2 x 8192 20.9, 15.4; 1 row 13.1, 14.9; 64 x 1000 -> 2 x 2728 8.6, 10.9):
 //   bfloat16   1 x 2048 -> 2 x 8192 (67 MB) 13.2, 15.1; 16 rows 15.6, 15.4; 16 x 4096 -> 2 x 8192 29.0, 25.5; 32 x 2048 ->
 //              2 x 4096 10.8, 11.4; 64 x 2048 -> 2 x 4096 15.1, 13.1; 64 x 1000 -> 2 x 2728 7.1, 9.5;
 //              16 x 8192 -> 2 x 2048 23.9, 16.1; 16 x 512 -> 2 x 16384 8.5, 6.8

@@ -37,8 +37,9 @@ MEASURED = [  # T, D, F, type: the fastest of the kernels that were timed for a 
     (700, 1024, 4096, BF, "128"), (1000, 1000, 4096, BF, "128"), (1000, 1024, 4096, BF, "128"), (600, 1024, 4096, BF, "128"),
     (520, 2048, 4096, BF, "128"), (400, 512, 6000, BF, "128"), (512, 1000, 4224, BF, "128"), (300, 1000, 7000, BF, "128"),
     (1500, 512, 3000, BF, "128"), (100, 1000, 17000, BF, "128"), (700, 2048, 4096, BF, "128"), (900, 1000, 3000, BF, "128"),
-    (520, 512, 4096, BF, "128"), (500, 512, 1365, F32, "64"),
-    (65, 4096, 16384, BF, "128"), (2048, 4096, 4096, BF, "256"),
+    (520, 512, 4096, BF, "128"),
+    # one set of operands over and over
+    (500, 512, 1365, F32, "64"), (65, 4096, 16384, BF, "128"), (2048, 4096, 4096, BF, "256"),
     (64, 1000, 2728, BF, "few"), (32, 2048, 4096, BF, "few"), (64, 2048, 4096, BF, "64"), (16, 4096, 8192, BF, "64"),
     (16, 8192, 2048, BF, "64"), (16, 512, 16384, BF, "64"), (16, 4096, 8192, F32, "few"), (32, 4096, 8192, F32, "64"),
     (64, 2047, 4096, F32, "few"), (64, 4095, 8191, F32, "few"), (1, 4095, 8191, BF, "few")]
